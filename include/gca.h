@@ -225,6 +225,131 @@ gca_status gca_forward_noalloc(const gca_problem* p, const void* lmk_q, const vo
                                int32_t* idx, float* sel, float* lse, float* w,
                                hipStream_t stream);
 
+/* ---------------------------------------------------------------- chunk cache ----
+ *
+ * A bounded cache of past chunks in 8 bits, for serving: every sequence has `capacity`
+ * slots of one chunk (up to S tokens).  The calls below store chunks into slots, select
+ * the slots to attend to by landmark, attend to them, and evict the chunks that were
+ * attended to least.  All state is the caller's device memory, named in gca_cache; every
+ * call reads lengths, slots and counters on the device, so a serving loop needs no
+ * synchronisation and can be captured into a HIP graph.
+ *
+ * GCA has no positions between chunks (Methodology: retrieved chunks are attended to one
+ * by one), so a chunk may sit in any slot; ties between scores go to the lower slot.
+ *
+ * Numbers.  A cached number stands for itself times its tile's scale; a tile is the keys
+ * or the values of one chunk of one cached head.
+ *   GCA_E4M3  8-bit floats (OCP e4m3, 4 exponent and 3 mantissa bits, largest 448); the
+ *             scale is the least power of two (at least 2^-126) that brings the tile's largest
+ *             finite magnitude to at most 448.  Infinities are stored as +-448, NaN as NaN.
+ *   GCA_INT8  integers -127 .. 127; the scale is the largest finite magnitude (at least
+ *             2^-100) over 127.  Infinities are stored as +-127; a tile with a NaN gets the
+ *             scale NaN.
+ * Values are stored transposed, so that both products of the attention read their operand
+ * from memory in the order in which the matrix cores take it.
+ */
+typedef enum { GCA_E4M3 = 0, GCA_INT8 = 1 } gca_format;
+
+/* B sequences; H query heads share Hkv cached heads (query head h reads cached head
+ * h / (H / Hkv)); Hr = 1 list of slots per sequence, or Hr = Hkv, one per cached head.
+ * Supported: d == 64, S == 64, H a multiple of Hkv, 1 <= capacity <= 262144, 1 <= topk
+ * <= 32, D a positive multiple of 64 up to 8192.  A call requires the members it names. */
+typedef struct {
+  int32_t B, H, Hkv, Hr;
+  int32_t d, S;
+  int64_t capacity;     /* slots per sequence */
+  int32_t topk;         /* entries of a list of slots, 1..32 */
+  int32_t D;            /* landmark vector width */
+  float score_scale;    /* multiplies <landmark query, landmark key> */
+  float attn_scale;     /* multiplies <q, k> */
+  int32_t off_by_one;   /* as in gca_problem */
+  int32_t dtype;        /* gca_dtype of q, k, v, out, lmk and landmark queries */
+  int32_t format;       /* gca_format of the cached numbers */
+  uint32_t flags;       /* 0 */
+  void* k;              /* [B, Hkv, capacity, S, d] 8-bit keys */
+  void* v;              /* [B, Hkv, capacity, d, S] 8-bit values, transposed per chunk */
+  float* k_scale;       /* [B, Hkv, capacity] */
+  float* v_scale;       /* [B, Hkv, capacity] */
+  void* lmk;            /* [B, Hr, capacity, D] dtype: landmark keys */
+  int32_t* tokens;      /* [B, capacity] tokens of the chunk in each slot; <= 0: the slot is free */
+  float* mass;          /* [B, capacity] attention weight that the chunk has gathered */
+  int32_t* number;      /* [B, capacity] the chunk's number in its sequence */
+  int32_t* next;        /* [B] number of the sequence's next chunk */
+} gca_cache;
+
+/* Store chunk i of sequence b, tokens 64 i .. 64 i + 63 of the new keys and values, into
+ * slot slots[b, i]: quantised tiles and scales, its length into `tokens`, its landmark key
+ * into `lmk`.  Rows behind a chunk's last token are stored as zeros.  Entries outside
+ * [0, capacity) and chunks without tokens are skipped, and nothing of any other slot is
+ * written.  Where a sequence names a slot twice, its last chunk with tokens is stored.
+ *   k, v    [B, Hkv, n * S, d] dtype
+ *   lmk     [B, Hr, n, D]      dtype    landmark keys; NULL: c->lmk is left as it is
+ *   slots   [B, n]             int32    (e.g. from gca_cache_evict)
+ *   lengths [B]                int32    new tokens of each sequence, at most n * S of which
+ *                                       count; NULL: n * S
+ * Requires c->k, v, k_scale, v_scale, tokens, and lmk if the argument is given. */
+gca_status gca_cache_store(const gca_cache* c, const void* k, const void* v, const void* lmk,
+                           const int32_t* slots, const int32_t* lengths, int64_t n, hipStream_t stream);
+
+/* Retrieval among the slots in use (Eq. 1, as DECODE mode): for each retrieval row the
+ * min(topk, #candidates) best scores score_scale * <lmk_q, lmk[slot]>, where candidates
+ * are the slots with tokens > 0 whose score is finite; ties go to the lower slot.
+ *   lmk_q [B, Hr, 1, D]    dtype
+ *   idx   [B, Hr, 1, topk] int32  output: slots ascending, -1 padded
+ *   sel   [B, Hr, 1, topk] fp32   output: their scores, -inf padded
+ *   w     [B, Hr, 1, topk] fp32   output: softmax of sel (Eq. 2), 0 on pads; may be NULL
+ * Requires c->lmk and tokens.  Workspace: gca_cache_workspace_size(c,
+ * GCA_OP_CACHE_SELECT, 0) bytes, 256-byte aligned. */
+gca_status gca_cache_select(const gca_cache* c, const void* lmk_q, int32_t* idx, float* sel, float* w,
+                            void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Grouped cross attention over the cache (Eq. 2-3; as gca_grouped_xattn_fwd).  The query
+ * rows come in nQ groups of `rows` rows (one token, a few, a chunk, or any number), and
+ * group t attends to the chunks of list t - lag: lag = 0 gives every group the list of its
+ * own number, lag = 1 the one before (CAUSAL lists; group 0 then has none).  Entries that
+ * name no slot in use (outside [0, capacity), or tokens <= 0) are pads; a slot's softmax
+ * is over its first `tokens` keys.  Rows without a valid entry get out = 0.
+ *   q   [B, H, nQ * rows, d]    dtype
+ *   idx [B, Hr, nQ, topk]       int32
+ *   sel [B, Hr, nQ, topk]       fp32   finite on valid entries
+ *   out [B, H, nQ * rows, d]    dtype  output
+ *   lse [B, H, nQ * rows, topk] fp32   output: log of each entry's softmax denominator
+ *                                      (-inf on pads), may be NULL
+ *   w   [B, Hr, nQ, topk]       fp32   output: fusion weights of every list, may be NULL
+ * Products of q with the cached numbers are exact and summed in fp32; probabilities are
+ * rounded to fp16 (fp32 tensors: to two fp16 terms) before they meet the values.
+ * Requires c->k, v, k_scale, v_scale, tokens. */
+gca_status gca_cache_xattn(const gca_cache* c, const void* q, const int32_t* idx, const float* sel, void* out,
+                           float* lse, float* w, int64_t nQ, int64_t rows, int32_t lag, hipStream_t stream);
+
+/* Make room for the n next chunks of every sequence by evicting the chunks that gathered
+ * the least attention weight.  In this order, for each sequence b:
+ *   1. mass[b, j] = decay * mass[b, j] + the weights w of the entries of its lists that name
+ *      slot j, for slots in use (each weight counted to the nearest 2^-48, negative and NaN
+ *      ones as 0, so that the sum does not depend on its order); 0 for free slots;
+ *   2. m = want[b] slots (n if want is NULL; at most n) are taken: free slots first, lowest
+ *      first, then the chunks in order of (mass, slot), except those numbered below
+ *      keep_first or not below next[b] - keep_last.  A negative or NaN mass ranks as 0;
+ *   3. the slots taken are written to slots[b, 0 ..], ascending, padded with -1 where there
+ *      are fewer than n; tokens and mass of each become 0 and number[b, slots[b, i]] =
+ *      next[b] + i; then next[b] += m.
+ * gca_cache_store then fills them.  With n = 0 only the masses change.
+ *   idx, w [B, Hr, nQ, topk] int32, fp32  lists and fusion weights since the last call; both
+ *                                         NULL (and nQ ignored): none
+ *   want   [B]               int32        may be NULL
+ *   slots  [B, n]            int32        output
+ * Requires c->tokens, mass, number, next.  Workspace: gca_cache_workspace_size(c,
+ * GCA_OP_CACHE_EVICT, n) bytes (0 for small caches), 256-byte aligned. */
+gca_status gca_cache_evict(const gca_cache* c, const int32_t* idx, const float* w, int64_t nQ, float decay,
+                           int32_t keep_first, int32_t keep_last, const int32_t* want, int32_t* slots, int64_t n,
+                           void* workspace, size_t ws_bytes, hipStream_t stream);
+
+#define GCA_OP_CACHE_SELECT 2
+#define GCA_OP_CACHE_EVICT 3
+/* Bytes of workspace `op` (GCA_OP_CACHE_SELECT, or GCA_OP_CACHE_EVICT of n chunks) needs;
+ * 0 if c is invalid or needs none.  It depends on c's sizes alone and never falls as n grows. */
+size_t gca_cache_workspace_size(const gca_cache* c, int op, int64_t n);
+
 /* Profiling aid (outside the method).  While armed, the i-th kernel that libgca
  * launches from the calling thread (i = 0, 1, ... while 2 (i + 1) <= capacity,
  * capacity <= 4096) is dispatched with events[2 i] and events[2 i + 1] as its

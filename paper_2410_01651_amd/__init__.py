@@ -5,4 +5,4 @@ The compute lives in ``libgca.so`` (HIP kernels behind the C ABI declared in
 """
 
 from . import gca  # noqa: F401
-from .gca import GcaError, Problem, problem  # noqa: F401
+from .gca import Cache, GcaError, Problem, cache, problem  # noqa: F401

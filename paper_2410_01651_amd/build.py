@@ -18,8 +18,9 @@ INCLUDE = os.path.join(ROOT, "include")
 OUT = os.path.join(HERE, "libgca.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
-SOURCES = ["api.cpp", "plan.cpp", "noalloc.hip", "scores.hip", "select.hip", "xattn_fwd.hip", "xattn_decode.hip",
-           "xattn_bwd.hip"]
+SOURCES = ["api.cpp", "cache_api.cpp", "plan.cpp", "noalloc.hip", "scores.hip", "cache_select.hip", "select.hip",
+           "xattn_fwd.hip", "xattn_decode.hip", "xattn_bwd.hip", "cache_store.hip", "cache_xattn.hip",
+           "cache_evict.hip"]
 # The attention kernels never rely on NaN semantics: without IEEE mode the
 # softmax max needs no operand canonicalisation, and MFMA accumulators in
 # ordinary VGPRs need no copies out of the accumulation registers.
@@ -27,6 +28,7 @@ PER_SOURCE = {
     "xattn_fwd.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
     "xattn_decode.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
     "xattn_bwd.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "cache_xattn.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 ARCH = "gfx950"
 

@@ -8,7 +8,13 @@
 #include <cstdlib>
 #include <string>
 
+#include "gca_check.hpp"
 #include "gca_plan.hpp"
+
+using gca::check_ptr;
+using gca::check_ws;
+using gca::fail;
+using gca::from_hip;
 
 namespace {
 
@@ -21,19 +27,6 @@ struct ProfileHook {
   const char* names[4096];
 };
 thread_local ProfileHook g_profile;
-
-gca_status fail(gca_status s, const std::string& msg) {
-  g_last_error = msg;
-  return s;
-}
-
-gca_status from_hip(hipError_t e, const char* what) {
-  if (e == hipSuccess) return GCA_OK;
-  std::string msg = std::string(what) + ": " + hipGetErrorString(e);
-  const char* kernel = gca::launch_error_kernel();
-  if (kernel[0]) msg += std::string(" (kernel ") + kernel + ")";
-  return fail(GCA_ERR_HIP, msg);
-}
 
 constexpr int64_t kMaxGrid = 2147483647;  // largest 1-D grid we launch
 
@@ -113,19 +106,6 @@ gca_status device_view(const gca_problem* p, const void*& ptr, const char* name)
   return GCA_OK;
 }
 
-gca_status check_ptr(const void* ptr, const char* name, bool required, unsigned align) {
-  if (!ptr) return required ? fail(GCA_ERR_INVALID, std::string(name) + " is NULL") : GCA_OK;
-  if (reinterpret_cast<uintptr_t>(ptr) % align)
-    return fail(GCA_ERR_INVALID, std::string(name) + " is not " + std::to_string(align) + "-byte aligned");
-  return GCA_OK;
-}
-
-#define GCA_TRY(expr)               \
-  do {                              \
-    const gca_status st_ = (expr);  \
-    if (st_ != GCA_OK) return st_;  \
-  } while (0)
-
 // Causal selection without the score matrix when asked to, or when the matrix
 // would exceed 256 MiB (unless the caller insists on materialising it).
 bool fused_path(const gca_problem* p, const gca::Shape& s) {
@@ -161,6 +141,29 @@ void* wide_scratch(const gca::Shape& s, const void* lmk_q, const void* lmk_k, co
              : nullptr;
 }
 
+}  // namespace
+
+namespace gca {
+gca_status fail(gca_status s, const std::string& msg) {
+  g_last_error = msg;
+  return s;
+}
+
+gca_status from_hip(hipError_t e, const char* what) {
+  if (e == hipSuccess) return GCA_OK;
+  std::string msg = std::string(what) + ": " + hipGetErrorString(e);
+  const char* kernel = launch_error_kernel();
+  if (kernel[0]) msg += std::string(" (kernel ") + kernel + ")";
+  return fail(GCA_ERR_HIP, msg);
+}
+
+gca_status check_ptr(const void* ptr, const char* name, bool required, unsigned align) {
+  if (!ptr) return required ? fail(GCA_ERR_INVALID, std::string(name) + " is NULL") : GCA_OK;
+  if (reinterpret_cast<uintptr_t>(ptr) % align)
+    return fail(GCA_ERR_INVALID, std::string(name) + " is not " + std::to_string(align) + "-byte aligned");
+  return GCA_OK;
+}
+
 gca_status check_ws(void* ws, size_t have, size_t need) {
   if (need == 0) return GCA_OK;
   if (!ws) return fail(GCA_ERR_WORKSPACE, "workspace is NULL, need " + std::to_string(need) + " bytes");
@@ -171,9 +174,6 @@ gca_status check_ws(void* ws, size_t have, size_t need) {
   return GCA_OK;
 }
 
-}  // namespace
-
-namespace gca {
 thread_local hipError_t g_launch_error = hipSuccess;
 thread_local const char* g_launch_error_kernel = "";
 thread_local const char* g_reported_kernel = "";

@@ -1,0 +1,477 @@
+// Grouped cross attention over the 8-bit chunk cache (gca_cache_xattn): Eq. 2-3 for groups of
+// any number of query rows, each group with its own list of slots.
+//
+// Mathematics.  For slot j of a list, K_j = kappa_j N_j and V_j = nu_j M_j with 8-bit numbers
+// N, M, so  s = (attn_scale kappa_j) q N_j^T,  P = softmax(s) over the chunk's tokens, and
+// out = sum_j w_j P V_j = nu sum_j (w_j nu_j / nu) P M_j  with nu the largest of the list's
+// nu_j.  Every e4m3 number and every int8 is exact in bf16 and in fp16, so the scales stay out
+// of the operands: q N^T is a product of exact operands with fp32 sums (fp32 queries: three
+// bf16 terms, 24 bits), and the scaled probabilities (w_j nu_j / nu) P 2^15 <= 2^15 meet M in
+// fp16, 11 bits each (fp32 tensors: two fp16 terms, 22 bits).  As every chunk has a softmax of its own,
+// nothing is rescaled and the slots of a list can be split over waves and added.
+//
+// Layout.  The products are formed transposed, S^T = N Q^T and O^T = M^T P^T, on MFMA tiles of
+// W x W (W = 32, or 16 for at most 16 rows): lane l = W g + c has query row c as its column.
+// Row m of block a of N is not token W a + m but the token that makes a lane's accumulators
+// consecutive tokens (`tile_row`): W = 32: 32 a + 16 g + (0..15); W = 16: 16 g + (0..15).  They are
+// then, rounded, the operand of the second product as they stand, and what a lane needs of M
+// (stored transposed: columns of a chunk's values are rows) are 16 consecutive bytes; so are
+// its columns of N.  A tile is 4 loads of 16 bytes per lane straight from the cache into
+// registers, unpacked two numbers per instruction (e4m3), with neither LDS nor a transpose.
+// The same order of M's rows leaves a lane 16 consecutive columns of the output.
+//
+// Work.  One workgroup per (sequence, cached head, group, block of rows); its waves take the
+// list's valid slots in turn.
+#include "cache_plan.hpp"
+#include "gca_device.hpp"
+#include "gca_launch.hpp"
+
+namespace gca {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+constexpr int kMaxWaves = 8;
+constexpr int kTileBytes = kS * kD;
+
+struct XattnParams {
+  const uint8_t* k;
+  const uint8_t* v;
+  const float* ks;
+  const float* vs;
+  const int32_t* tokens;
+  const void* q;
+  const int32_t* idx;
+  const float* sel;
+  void* out;
+  float* lse;
+  float* w;
+  uint32_t items, blocks;  // work items; row blocks per group
+  uint32_t nQ, H, Hkv, Hr, G, rows, M;  // M = G rows: query rows of a group that share a cached head
+  uint32_t part;  // bytes of LDS before the partial outputs
+  int topk, lag, off_by_one, C;
+  float scale;  // |attn_scale| log2 e
+  int negate;   // attn_scale < 0: the queries' signs are turned
+};
+
+__device__ __forceinline__ f32x16 mma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const f16x8& a, const f16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(const f16x8& a, const f16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight numbers (dwords x, y) as a bf16 / fp16 operand, exactly.
+template <bool I8>
+__device__ __forceinline__ bf16x8 to_bf16(uint32_t x, uint32_t y) {
+  if constexpr (I8) {
+    bf16x8 f;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      f[m] = (__bf16)(float)(int8_t)(x >> (8 * m));
+      f[4 + m] = (__bf16)(float)(int8_t)(y >> (8 * m));
+    }
+    return f;
+  } else {
+    const u32x4 r = u32x4{
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.f, false)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.f, true))};
+    return __builtin_bit_cast(bf16x8, r);
+  }
+}
+template <bool I8>
+__device__ __forceinline__ f16x8 to_f16(uint32_t x, uint32_t y) {
+  if constexpr (I8) {
+    // n + 128 in the low mantissa bits of 1024: fp16 1152 + n
+    auto two = [](uint32_t u, uint32_t sel) {
+      const f16x2 m = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, sel));
+      return __builtin_bit_cast(uint32_t, m - f16x2{(_Float16)1152, (_Float16)1152});
+    };
+    x ^= 0x80808080u;
+    y ^= 0x80808080u;
+    return __builtin_bit_cast(
+        f16x8, u32x4{two(x, 0x04010400), two(x, 0x04030402), two(y, 0x04010400), two(y, 0x04030402)});
+  } else {
+    const u32x4 r = u32x4{
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, false)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y, 1.f, false)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y, 1.f, true))};
+    return __builtin_bit_cast(f16x8, r);
+  }
+}
+
+// T: type of the queries; W: MFMA tile; NC: column blocks of W query rows.
+template <typename T, bool I8, int W, int NC>
+__global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnParams p) {
+  constexpr bool kB16 = sizeof(T) == 2;
+  constexpr int NG = 64 / W;           // lane groups
+  constexpr int NA = 64 / W;           // blocks of W tokens (or columns) per tile
+  constexpr int NK = W / 8;            // steps of the contraction over 64 columns (or tokens)
+  constexpr int NX = NK / 2;           // 16-byte pieces per lane and block
+  constexpr int NR = W * W / 64;       // accumulators per block
+  constexpr int NV = NA * NR;          // values per lane and column block
+  constexpr int QP = kB16 ? 1 : 3;     // bf16 terms of a query entry
+  constexpr int PP = kB16 ? 1 : 2;     // fp16 terms of a probability
+  constexpr int QB = W * NC;           // query rows per item
+  typedef __attribute__((ext_vector_type(NR))) float Acc;
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+
+  const uint32_t it = (uint32_t)xcd_swizzle(blockIdx.x, gridDim.x);
+  if (it >= p.items) return;
+  const int lane = threadIdx.x & 63, g = lane / W, col = lane % W;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
+  // item = ((b Hkv + h) nQ + t) blocks + block
+  const uint32_t blk = it % p.blocks, bt = it / p.blocks, t = bt % p.nQ, bh = bt / p.nQ, h = bh % p.Hkv, b = bh / p.Hkv;
+  const int K = p.topk;
+
+  // ---- the list: lane s holds entry s.  Groups before the first list take the weights of
+  // the last one, which feeds no group.
+  const bool has_list = (int)t >= p.lag;
+  const uint32_t list = has_list ? t - p.lag : p.nQ - 1;
+  const int64_t row = ((int64_t)b * p.Hr + (p.Hr == 1 ? 0 : h)) * p.nQ + list;
+  int j = -1;
+  float sv = -INFINITY;
+  if (lane < K) {
+    j = p.idx[row * K + lane];
+    sv = p.sel[row * K + lane];
+  }
+  const bool named = j >= 0 && j < p.C;
+  j = named ? j : 0;
+  const int length = named ? min(p.tokens[(int64_t)b * p.C + j], kS) : 0;
+  const int64_t slot0 = (int64_t)bh * p.C;
+  const float kscale = named ? p.ks[slot0 + j] : 0.f;
+  float vscale = named ? p.vs[slot0 + j] : 0.f;
+
+  // ---- the queries: lane (g, c) takes columns 16 (g + NG x) .. of row c, x < NX
+  const uint32_t m0 = blk * QB;
+  const bool flat = p.G == 1 || p.nQ == 1;  // a group's rows are consecutive
+  const int64_t row0 = ((int64_t)(b * p.H + h * p.G) * p.nQ + t) * p.rows;
+  auto q_row = [&](uint32_t m) -> int64_t {
+    return row0 + (flat ? m : (int64_t)(m / p.rows) * p.nQ * p.rows + m % p.rows);
+  };
+  bf16x8 qf[NC][NK][QP];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const uint32_t m = min(m0 + c * W + col, p.M - 1);
+    const T* qr = reinterpret_cast<const T*>(p.q) + q_row(m) * kD;
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      const T* src = qr + 16 * (g + NG * (s >> 1)) + 8 * (s & 1);
+      if constexpr (kB16) {
+        u32x4 x = *reinterpret_cast<const u32x4*>(src);
+        if (p.negate) x ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+        qf[c][s][0] = __builtin_bit_cast(bf16x8, x);
+      } else {
+#pragma unroll
+        for (int m8 = 0; m8 < 8; ++m8) {
+          float x = src[m8];
+          if (p.negate) x = -x;
+#pragma unroll
+          for (int e = 0; e < QP; ++e) {
+            const __bf16 part = (__bf16)x;
+            qf[c][s][e][m8] = part;
+            x -= (float)part;
+          }
+        }
+      }
+    }
+  }
+
+  // ---- fusion weights (Eq. 2)
+  const bool valid = length > 0;
+  vscale = valid ? vscale : 0.f;  // (a free slot's scale may be anything)
+  const float top = max64(valid ? sv : -INFINITY);
+  const float es = valid ? expf(sv - top) : 0.f;
+  const float total = sum64(es);
+  const float wl = valid ? es / total : 0.f;
+  if (p.w && wave == 0 && blk == 0 && (p.Hr != 1 || h == 0) && lane < K) p.w[row * K + lane] = wl;
+  const float vmax = max64(vscale);
+  const float coef = vmax > 0.f ? wl * (vscale / vmax) * 0x1p15f : wl * vscale;
+  // this wave's entries: those whose rank among the valid ones is wave (mod nw)
+  const uint64_t all = __ballot(valid && has_list);
+  const uint32_t count = __popcll(all);
+  uint32_t mine = (uint32_t)__ballot(valid && has_list && ((uint32_t)lanes_below(all) & (nw - 1)) == wave);
+
+  const uint32_t nrows = min((uint32_t)QB, p.M - m0);
+  float* const lse_s = smem;  // [row][entry]
+  if (p.lse) {
+    for (uint32_t e = threadIdx.x; e < nrows * K; e += blockDim.x) lse_s[e] = -INFINITY;
+    __syncthreads();
+  }
+
+  // piece (a, x) of a tile: row tile_row(a) = the token (column) of this lane's operand row,
+  // bytes 16 (g + NG x) ..
+  const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
+                                    : 16 * (col >> 2) + (col & 3);
+  const uint32_t lane_off = lane_row * kD + 16 * g;
+  auto load_tile = [&](u32x4* x, const uint8_t* base, int slot) {
+    const uint8_t* tile = base + (slot0 + slot) * kTileBytes;
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+        x[a * NX + y] =
+            *reinterpret_cast<const u32x4*>(tile + lane_off + (W == 32 ? 32 : 4) * a * kD + 16 * NG * y);
+  };
+
+  Acc o[NC][NA];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int a = 0; a < NA; ++a) o[c][a] = Acc{};
+
+  u32x4 kr[NA * NX], vr[NA * NX];
+  if (mine != 0) {
+    const int jn = __builtin_amdgcn_readlane(j, __builtin_ctz(mine));
+    load_tile(kr, p.k, jn);
+    load_tile(vr, p.v, jn);
+  }
+  while (mine != 0) {
+    const int s = __builtin_ctz(mine);
+    mine &= mine - 1;
+    const int jn = mine != 0 ? __builtin_amdgcn_readlane(j, __builtin_ctz(mine)) : 0;
+    const int len = __builtin_amdgcn_readlane(length, s);
+    const float sc = p.scale * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kscale), s));
+    const float cf = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(coef), s));
+
+    // S^T = N Q^T
+    Acc st[NC][NA];
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) st[c][a] = Acc{};
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const u32x4 r = kr[a * NX + (i >> 1)];
+        const bf16x8 f = to_bf16<I8>(r[2 * (i & 1)], r[2 * (i & 1) + 1]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < QP; ++e) st[c][a] = mma(f, qf[c][i][e], st[c][a]);
+      }
+    }
+    if (mine != 0) load_tile(kr, p.k, jn);
+
+    // softmax over the chunk's tokens; value u of a lane is token 32 (u / 16) + 16 g + u % 16
+    // (W = 32) or 16 g + u (W = 16)
+    f16x8 pf[NC][NK][PP];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float v[NV];
+#pragma unroll
+      for (int u = 0; u < NV; ++u) v[u] = st[c][u / NR][u % NR];
+      if (len < kS) {
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+          if ((W == 32 ? 32 * (u / 16) + u % 16 : u) + 16 * g >= len) v[u] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(v[0], v[1]), v[2]), mx2 = fmaxf(fmaxf(v[3], v[4]), v[5]);
+#pragma unroll
+      for (int u = 6; u + 3 < NV; u += 4) {
+        mx = fmaxf(fmaxf(mx, v[u]), v[u + 1]);
+        mx2 = fmaxf(fmaxf(mx2, v[u + 2]), v[u + 3]);
+      }
+      mx = fmaxf(fmaxf(mx, v[NV - 2]), fmaxf(mx2, v[NV - 1]));
+      if constexpr (W == 16) {
+        uint32_t x, y;
+        pair16(__float_as_uint(mx), x, y);
+        mx = fmaxf(__uint_as_float(x), __uint_as_float(y));
+      }
+      mx = max_xor32(mx) * sc;
+      if (p.off_by_one) mx = fmaxf(mx, 0.f);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) v[u] = __builtin_amdgcn_exp2f(fmaf(v[u], sc, -mx));
+      if (len < kS) {  // (a scale of zero times -inf)
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+          if ((W == 32 ? 32 * (u / 16) + u % 16 : u) + 16 * g >= len) v[u] = 0.f;
+      }
+      float sum = v[0], sum2 = v[1];
+#pragma unroll
+      for (int u = 2; u < NV; u += 2) {
+        sum += v[u];
+        sum2 += v[u + 1];
+      }
+      sum += sum2;
+      if constexpr (W == 16) {
+        uint32_t x, y;
+        pair16(__float_as_uint(sum), x, y);
+        sum = __uint_as_float(x) + __uint_as_float(y);
+      }
+      sum = sum_xor32(sum);
+      if (p.off_by_one) sum += __builtin_amdgcn_exp2f(-mx);
+      if (p.lse && g == 0 && (uint32_t)(c * W + col) < nrows)
+        lse_s[(c * W + col) * K + s] = (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+      const float f = cf * __builtin_amdgcn_rcpf(sum);
+#pragma unroll
+      for (int i = 0; i < NK; ++i)
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+          float x = v[8 * i + m] * f;
+          // (one rounding of x: the first term's and the second's must be the same number)
+          if constexpr (PP == 2) asm("" : "+v"(x));
+          const _Float16 hi = (_Float16)x;
+          pf[c][i][0][m] = hi;
+          if constexpr (PP == 2) pf[c][i][PP - 1][m] = (_Float16)(x - (float)hi);
+        }
+    }
+
+    // O^T += M^T P^T (numbers behind the chunk's last token are cleared: a masked NaN stays out)
+    if (len < kS) {
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const int left = len - (16 * (g + NG * y) + 4 * d);
+          const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+          for (int a = 0; a < NA; ++a) vr[a * NX + y][d] &= keep;
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const u32x4 r = vr[a * NX + (i >> 1)];
+        const f16x8 f = to_f16<I8>(r[2 * (i & 1)], r[2 * (i & 1) + 1]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < PP; ++e) o[c][a] = mma(f, pf[c][i][e], o[c][a]);
+      }
+    if (mine != 0) load_tile(vr, p.v, jn);
+  }
+
+  // ---- output: value u of a lane is column 32 (u / 16) + 16 g + u % 16 (W = 32) or 16 g + u
+  const float osc = vmax > 0.f ? vmax * 0x1p-15f : 1.f;
+  if (nw == 1) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const uint32_t m = c * W + col;
+      if (m >= nrows) continue;
+      T* dst = reinterpret_cast<T*>(p.out) + q_row(m0 + m) * kD + 16 * g;
+#pragma unroll
+      for (int u = 0; u < NV; u += 4) {
+        const Acc& a = o[c][u / NR];
+        store4(dst + (u / 16) * 32 + u % 16, a[u % NR] * osc, a[u % NR + 1] * osc, a[u % NR + 2] * osc,
+               a[u % NR + 3] * osc);
+      }
+    }
+    if (p.lse) __syncthreads();
+  } else {
+    // the waves' partial sums: part[wave][row][16 blocks of 4], block x of row r at x ^ (r mod 16)
+    float* const part = smem + p.part / sizeof(float);
+    const uint32_t waves = min(nw, count);
+    if (wave < waves) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const uint32_t m = c * W + col;
+        if (m >= nrows) continue;
+        float* pr = part + (wave * nrows + m) * kD;
+#pragma unroll
+        for (int u = 0; u < NV; u += 4) {
+          const Acc& a = o[c][u / NR];
+          const uint32_t x = (4 * g + (u / 16) * 8 + (u % 16) / 4) ^ (m & 15);
+          *reinterpret_cast<f32x4*>(pr + 4 * x) =
+              f32x4{a[u % NR], a[u % NR + 1], a[u % NR + 2], a[u % NR + 3]};
+        }
+      }
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < nrows * 16; e += blockDim.x) {
+      const uint32_t m = e >> 4, x = e & 15;
+      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (uint32_t y = 0; y < waves; ++y)
+        acc += *reinterpret_cast<const f32x4*>(part + (y * nrows + m) * kD + 4 * (x ^ (m & 15)));
+      store4(reinterpret_cast<T*>(p.out) + q_row(m0 + m) * kD + 4 * x, acc[0] * osc, acc[1] * osc, acc[2] * osc,
+             acc[3] * osc);
+    }
+  }
+  if (p.lse) {
+    for (uint32_t e = threadIdx.x; e < nrows * K; e += blockDim.x) {
+      const uint32_t m = e / K;
+      p.lse[q_row(m0 + m) * K + (e - m * K)] = lse_s[e];
+    }
+  }
+}
+
+// Rows per item: 16 where the group has no more; 32; 64 in bf16 (both halves share a tile's
+// unpacking; fp32 queries in three terms leave no registers for it).
+int rows_per_item(const gca_cache& c, int64_t M) {
+  if (M <= 16) return 16;
+  return M <= 32 || c.dtype != GCA_BF16 ? 32 : 64;
+}
+
+}  // namespace
+
+int64_t xattn_items(const gca_cache& c, int64_t nQ, int64_t rows) {
+  const int64_t M = (int64_t)(c.H / c.Hkv) * rows, per = rows_per_item(c, M);
+  return (int64_t)c.B * c.Hkv * nQ * ((M + per - 1) / per);
+}
+
+hipError_t launch_cache_xattn(const gca_cache& c, const void* q, const int32_t* idx, const float* sel, void* out,
+                              float* lse, float* w, int64_t nQ, int64_t rows, int lag, hipStream_t stream) {
+  const int64_t M = (int64_t)(c.H / c.Hkv) * rows;
+  const int qb = rows_per_item(c, M);
+  XattnParams p;
+  p.k = static_cast<const uint8_t*>(c.k);
+  p.v = static_cast<const uint8_t*>(c.v);
+  p.ks = c.k_scale;
+  p.vs = c.v_scale;
+  p.tokens = c.tokens;
+  p.q = q;
+  p.idx = idx;
+  p.sel = sel;
+  p.out = out;
+  p.lse = lse;
+  p.w = w;
+  p.items = (uint32_t)xattn_items(c, nQ, rows);
+  p.blocks = (uint32_t)((M + qb - 1) / qb);
+  p.nQ = (uint32_t)nQ;
+  p.H = c.H;
+  p.Hkv = c.Hkv;
+  p.Hr = c.Hr;
+  p.G = c.H / c.Hkv;
+  p.rows = (uint32_t)rows;
+  p.M = (uint32_t)M;
+  p.topk = c.topk;
+  p.lag = lag;
+  p.off_by_one = c.off_by_one;
+  p.C = (int)c.capacity;
+  p.scale = fabsf(c.attn_scale) * kLog2e;
+  p.negate = c.attn_scale < 0.f;
+  const int rb = (int)(M < qb ? M : qb);
+  p.part = lse ? (uint32_t)((rb * c.topk * sizeof(float) + 15) & ~size_t(15)) : 0u;
+  // Waves per item: enough to fill the chip's eight waves per CU, no more than the list has
+  // entries, and at most 64 KiB of LDS.
+  int nw = 1;
+  while (nw < kMaxWaves && 2 * nw <= c.topk && (int64_t)p.items * nw < 8 * device_cus() &&
+         p.part + 2 * nw * rb * kD * sizeof(float) <= 65536)
+    nw *= 2;
+  const size_t lds = p.part + (nw > 1 ? (size_t)nw * rb * kD * sizeof(float) : 0);
+  const dim3 grid((p.items + 7) / 8 * 8), block(64 * nw);
+  auto run = [&](auto tag, auto i8) {
+    using T = decltype(tag);
+    constexpr bool I8 = decltype(i8)::value;
+    if (qb == 16) launch_kernel("cache_xattn_kernel", cache_xattn_kernel<T, I8, 16, 1>, grid, block, lds, stream, p);
+    else if (qb == 32) launch_kernel("cache_xattn_kernel", cache_xattn_kernel<T, I8, 32, 1>, grid, block, lds, stream, p);
+    else if constexpr (sizeof(T) == 2)
+      launch_kernel("cache_xattn_kernel", cache_xattn_kernel<T, I8, 32, 2>, grid, block, lds, stream, p);
+  };
+  if (c.dtype == GCA_BF16) c.format == GCA_INT8 ? run(__bf16{}, std::true_type{}) : run(__bf16{}, std::false_type{});
+  else c.format == GCA_INT8 ? run(float{}, std::true_type{}) : run(float{}, std::false_type{});
+  return take_launch_error();
+}
+
+}  // namespace gca

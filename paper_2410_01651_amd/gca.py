@@ -21,6 +21,11 @@ EXPORTS = (
     "gca_grouped_xattn_bwd",
     "gca_forward",
     "gca_forward_noalloc",
+    "gca_cache_store",
+    "gca_cache_select",
+    "gca_cache_xattn",
+    "gca_cache_evict",
+    "gca_cache_workspace_size",
     "gca_workspace_size",
     "gca_status_string",
     "gca_last_error",
@@ -34,6 +39,8 @@ GCA_FP32, GCA_BF16 = 0, 1
 GCA_CAUSAL, GCA_DECODE = 0, 1
 FLAG_FUSED_TOPK, FLAG_MATERIALIZE, FLAG_GUMBEL, FLAG_HOST_KV, FLAG_LMK_ROW = 1, 2, 4, 8, 16
 OP_FORWARD, OP_BACKWARD = 0, 1
+GCA_E4M3, GCA_INT8 = 0, 1
+CACHE_SELECT, CACHE_EVICT = 2, 3
 NOALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -68,6 +75,37 @@ class Problem(ctypes.Structure):
         return self.S + 1 if self.flags & FLAG_LMK_ROW else self.S
 
 
+class CacheStruct(ctypes.Structure):
+    """Mirror of ``gca_cache``."""
+
+    _fields_ = [
+        ("B", ctypes.c_int32),
+        ("H", ctypes.c_int32),
+        ("Hkv", ctypes.c_int32),
+        ("Hr", ctypes.c_int32),
+        ("d", ctypes.c_int32),
+        ("S", ctypes.c_int32),
+        ("capacity", ctypes.c_int64),
+        ("topk", ctypes.c_int32),
+        ("D", ctypes.c_int32),
+        ("score_scale", ctypes.c_float),
+        ("attn_scale", ctypes.c_float),
+        ("off_by_one", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("lmk", ctypes.c_void_p),
+        ("tokens", ctypes.c_void_p),
+        ("mass", ctypes.c_void_p),
+        ("number", ctypes.c_void_p),
+        ("next", ctypes.c_void_p),
+    ]
+
+
 class GcaError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(message)
@@ -86,6 +124,7 @@ def lib():
                                "`python -m paper_2410_01651_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
         vp, P = ctypes.c_void_p, ctypes.POINTER(Problem)
+        C, i64 = ctypes.POINTER(CacheStruct), ctypes.c_int64
         sig = {
             "gca_chunk_scores": [P, vp, vp, vp, vp],
             "gca_topk": [P, vp, vp, vp, vp],
@@ -94,11 +133,18 @@ def lib():
                                       vp, ctypes.c_size_t, vp],
             "gca_forward": [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
             "gca_forward_noalloc": [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp],
+            "gca_cache_store": [C, vp, vp, vp, vp, vp, i64, vp],
+            "gca_cache_select": [C, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
+            "gca_cache_xattn": [C, vp, vp, vp, vp, vp, vp, i64, i64, ctypes.c_int32, vp],
+            "gca_cache_evict": [C, vp, vp, i64, ctypes.c_float, ctypes.c_int32, ctypes.c_int32, vp, vp, i64, vp,
+                                ctypes.c_size_t, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = ctypes.c_int
+        L.gca_cache_workspace_size.argtypes = [C, ctypes.c_int, i64]
+        L.gca_cache_workspace_size.restype = ctypes.c_size_t
         L.gca_workspace_size.argtypes = [P, ctypes.c_int]
         L.gca_workspace_size.restype = ctypes.c_size_t
         L.gca_status_string.argtypes = [ctypes.c_int]
@@ -365,6 +411,209 @@ def forward_noalloc(p: Problem, lmk_q, lmk_k, q, k, v, out, idx, sel, lse=None, 
         _ptr(sel, "sel", torch.float32, sh.rows), _ptr(lse, "lse", torch.float32, sh.lse),
         _ptr(w, "w", torch.float32, sh.rows), _stream(stream)))
     return {"out": out, "idx": idx, "sel": sel, "lse": lse, "w": w}
+
+
+# -------------------------------------------------------------- chunk cache ----
+
+class Cache:
+    """A bounded 8-bit chunk cache (``gca_cache``): its sizes and its device tensors, which
+    are the program's own and may be read or, between calls, changed:
+
+    * ``k`` [B, Hkv, C, 64 tokens, 64], ``v`` [B, Hkv, C, 64, 64 tokens]: 8-bit numbers
+      (``torch.float8_e4m3fn`` or ``torch.int8``), values transposed per chunk;
+    * ``k_scale``, ``v_scale`` [B, Hkv, C] fp32: a number stands for itself times these;
+    * ``lmk`` [B, Hr, C, D]: landmark keys; ``tokens`` [B, C] int32: 0 = free slot;
+    * ``mass`` [B, C] fp32, ``number`` [B, C] int32, ``next`` [B] int32: what eviction goes by.
+
+    To give sequence b's place to another sequence, zero ``tokens[b]``, ``mass[b]`` and
+    ``next[b]``."""
+
+    NAMES = ("k", "v", "k_scale", "v_scale", "lmk", "tokens", "mass", "number", "next")
+
+    def __init__(self, struct, tensors, device, index):
+        self.struct = struct
+        self.ref = ctypes.byref(struct)
+        self.device = device
+        self.index = index    # the device's ordinal
+        self.elem = _torch().bfloat16 if struct.dtype == GCA_BF16 else _torch().float32
+        for name in self.NAMES:
+            setattr(self, name, tensors[name])
+
+
+def cache_shapes(B, Hkv, capacity, Hr, D):
+    """Shapes of a cache's tensors, by name."""
+    return dict(k=(B, Hkv, capacity, 64, 64), v=(B, Hkv, capacity, 64, 64), k_scale=(B, Hkv, capacity),
+                v_scale=(B, Hkv, capacity), lmk=(B, Hr, capacity, D), tokens=(B, capacity), mass=(B, capacity),
+                number=(B, capacity), next=(B,))
+
+
+def cache(B, H, capacity, topk, Hkv=None, Hr=1, D=None, score_scale=None, attn_scale=None, off_by_one=False,
+          dtype="bf16", format="e4m3", device="cuda", tensors=None) -> Cache:
+    """A cache of `capacity` chunks for each of B sequences, all slots free.  Hkv defaults to H, D
+    to H * 64, the scales to 1/sqrt(D) and 1/sqrt(64); ``format`` is "e4m3" or "int8".  Members
+    named in ``tensors`` are taken as they are instead of allocated."""
+    torch = _torch()
+    Hkv, D = H if Hkv is None else Hkv, H * 64 if D is None else D
+    elem = {"bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
+    num = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}[format]
+    types = dict(k=num, v=num, k_scale=torch.float32, v_scale=torch.float32, lmk=elem, tokens=torch.int32,
+                 mass=torch.float32, number=torch.int32, next=torch.int32)
+    sh = cache_shapes(B, Hkv, capacity, Hr, D)
+    given = dict(tensors or {})
+    if not set(given) <= set(sh):
+        raise ValueError(f"a cache has no tensors named {sorted(set(given) - set(sh))}")
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError("a cache lives in device memory")
+    if device.index is None:
+        device = next(iter(given.values())).device if given else torch.device("cuda", torch.cuda.current_device())
+    for name, t in given.items():
+        _ptr(t, name, types[name], sh[name])
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+    for name in sh:
+        if name not in given:
+            given[name] = torch.zeros(sh[name], dtype=types[name], device=device)
+    struct = CacheStruct(
+        B=B, H=H, Hkv=Hkv, Hr=Hr, d=64, S=64, capacity=capacity, topk=topk, D=D,
+        score_scale=1.0 / math.sqrt(D) if score_scale is None else score_scale,
+        attn_scale=0.125 if attn_scale is None else attn_scale, off_by_one=int(bool(off_by_one)),
+        dtype=GCA_BF16 if dtype == "bf16" else GCA_FP32, format=GCA_E4M3 if format == "e4m3" else GCA_INT8, flags=0,
+        **{name: given[name].data_ptr() for name in sh})
+    return Cache(struct, given, device, device.index)
+
+
+def cache_workspace_size(c: Cache, op: int, n: int = 0) -> int:
+    return int(lib().gca_cache_workspace_size(c.ref, op, n))
+
+
+def cache_workspace(c: Cache, op: int, n: int = 0):
+    """Workspace of CACHE_SELECT, or of CACHE_EVICT of up to n chunks, on the cache's device."""
+    size = cache_workspace_size(c, op, n)
+    return _torch().empty(max(size, 1), dtype=_torch().uint8, device=c.device), size
+
+
+def _on(c: Cache, stream):
+    """Context in which a cache's call allocates and launches: its device (and the given stream)."""
+    if stream is not None:
+        return _torch().cuda.stream(stream)
+    return _torch().cuda.device(c.index)
+
+
+def _cache_ptr(c: Cache, t, name, dtype, shape):
+    if t is None:
+        return None
+    if t.device != c.device:
+        raise ValueError(f"{name} must be on the cache's device {c.device}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _cache_stream(c: Cache, stream):
+    if stream is None:
+        return _torch().cuda.current_stream(c.index).cuda_stream
+    if stream.device != c.device:
+        raise ValueError(f"the stream is on {stream.device}, the cache on {c.device}")
+    return stream.cuda_stream
+
+
+def cache_store(c: Cache, k, v, lmk, slots, lengths=None, stream=None):
+    """gca_cache_store: chunks of k, v [B, Hkv, n * 64, 64] (and their landmark keys lmk
+    [B, Hr, n, D], or None) into slots [B, n]; lengths [B]: new tokens of each sequence."""
+    torch = _torch()
+    s = c.struct
+    if slots.dim() != 2:
+        raise ValueError("slots must have shape (B, n)")
+    n = slots.shape[1]
+    kv = (s.B, s.Hkv, n * 64, 64)
+    args = (_cache_ptr(c, k, "k", c.elem, kv), _cache_ptr(c, v, "v", c.elem, kv),
+            _cache_ptr(c, lmk, "lmk", c.elem, (s.B, s.Hr, n, s.D)), _cache_ptr(c, slots, "slots", torch.int32, (s.B, n)),
+            _cache_ptr(c, lengths, "lengths", torch.int32, (s.B,)))
+    st = _cache_stream(c, stream)
+    with _on(c, stream):
+        _check(lib().gca_cache_store(c.ref, *args, n, st))
+
+
+def cache_select(c: Cache, lmk_q, idx=None, sel=None, w=None, want_w=True, ws=None, stream=None):
+    """gca_cache_select: the best slots in use for landmark queries lmk_q [B, Hr, 1, D];
+    returns idx, sel, w [B, Hr, 1, topk]."""
+    torch = _torch()
+    s = c.struct
+    rows = (s.B, s.Hr, 1, s.topk)
+    qp = _cache_ptr(c, lmk_q, "lmk_q", c.elem, (s.B, s.Hr, 1, s.D))
+    st = _cache_stream(c, stream)
+    with _on(c, stream):
+        if idx is None:
+            idx = torch.empty(rows, dtype=torch.int32, device=c.device)
+        if sel is None:
+            sel = torch.empty(rows, dtype=torch.float32, device=c.device)
+        if w is None and want_w:
+            w = torch.empty(rows, dtype=torch.float32, device=c.device)
+        if ws is None:
+            ws = cache_workspace(c, CACHE_SELECT)[0]
+        _check(lib().gca_cache_select(c.ref, qp, _cache_ptr(c, idx, "idx", torch.int32, rows),
+                                      _cache_ptr(c, sel, "sel", torch.float32, rows),
+                                      _cache_ptr(c, w, "w", torch.float32, rows),
+                                      _cache_ptr(c, ws, "workspace", torch.uint8, ws.shape), ws.numel(), st))
+    return idx, sel, w
+
+
+def cache_xattn(c: Cache, q, idx, sel, out=None, lse=None, w=None, want_lse=True, want_w=True, causal=False,
+                stream=None):
+    """gca_cache_xattn: query rows q [B, H, nQ * rows, 64] against the chunks that their group's
+    list idx, sel [B, Hr, nQ, topk] names (causal: the list before); returns out, lse, w."""
+    torch = _torch()
+    s = c.struct
+    if q.dim() != 4 or idx.dim() != 4:
+        raise ValueError("q must have shape (B, H, nQ * rows, 64) and idx (B, Hr, nQ, topk)")
+    nQ, Lq = idx.shape[2], q.shape[2]
+    if nQ < 1 or Lq < 1 or Lq % nQ:
+        raise ValueError(f"q's {Lq} rows are not a positive multiple of idx's {nQ} lists")
+    qs, rows, ls = (s.B, s.H, Lq, 64), (s.B, s.Hr, nQ, s.topk), (s.B, s.H, Lq, s.topk)
+    args = (_cache_ptr(c, q, "q", c.elem, qs), _cache_ptr(c, idx, "idx", torch.int32, rows),
+            _cache_ptr(c, sel, "sel", torch.float32, rows))
+    st = _cache_stream(c, stream)
+    with _on(c, stream):
+        if out is None:
+            out = torch.empty(qs, dtype=c.elem, device=c.device)
+        if lse is None and want_lse:
+            lse = torch.empty(ls, dtype=torch.float32, device=c.device)
+        if w is None and want_w:
+            w = torch.empty(rows, dtype=torch.float32, device=c.device)
+        _check(lib().gca_cache_xattn(c.ref, *args, _cache_ptr(c, out, "out", c.elem, qs),
+                                     _cache_ptr(c, lse, "lse", torch.float32, ls),
+                                     _cache_ptr(c, w, "w", torch.float32, rows), nQ, Lq // nQ, int(bool(causal)), st))
+    return out, lse, w
+
+
+def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_last=1, want=None, slots=None, ws=None,
+                stream=None):
+    """gca_cache_evict: adds the weights w of the lists idx [B, Hr, nQ, topk] to the masses and
+    returns slots [B, n] for each sequence's next n chunks (want [B]: fewer for some)."""
+    torch = _torch()
+    s = c.struct
+    lists = tuple(idx.shape) if idx is not None else None
+    if lists is not None and (len(lists) != 4 or lists[2] < 1):
+        raise ValueError("idx must have shape (B, Hr, nQ, topk)")
+    nQ = lists[2] if lists is not None else 0
+    rows = (s.B, s.Hr, nQ, s.topk)
+    args = (_cache_ptr(c, idx, "idx", torch.int32, rows), _cache_ptr(c, w, "w", torch.float32, rows))
+    wp = _cache_ptr(c, want, "want", torch.int32, (s.B,))
+    st = _cache_stream(c, stream)
+    with _on(c, stream):
+        if slots is None:
+            slots = torch.empty((s.B, n), dtype=torch.int32, device=c.device)
+        if ws is None:
+            ws = cache_workspace(c, CACHE_EVICT, n)[0]
+        _check(lib().gca_cache_evict(c.ref, *args, nQ, decay, keep_first, keep_last, wp,
+                                     _cache_ptr(c, slots, "slots", torch.int32, (s.B, n)) if n else None, n,
+                                     _cache_ptr(c, ws, "workspace", torch.uint8, ws.shape), ws.numel(), st))
+    return slots
 
 
 # ---------------------------------------------------------------- profiling ----
