@@ -76,8 +76,8 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t x, uint32_t y) {
     bf16x8 f;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      f[m] = (__bf16)(float)(int8_t)(x >> (8 * m));
-      f[4 + m] = (__bf16)(float)(int8_t)(y >> (8 * m));
+      f[m] = (__bf16)(float)(int8_t)((int)x >> (8 * m));
+      f[4 + m] = (__bf16)(float)(int8_t)((int)y >> (8 * m));
     }
     return f;
   } else {
@@ -132,7 +132,11 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   const int lane = threadIdx.x & 63, g = lane / W, col = lane % W;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
   // item = ((b Hkv + h) nQ + t) blocks + block
-  const uint32_t blk = it % p.blocks, bt = it / p.blocks, t = bt % p.nQ, bh = bt / p.nQ, h = bh % p.Hkv, b = bh / p.Hkv;
+  // (the quotients are formed on the vector unit: back to scalar registers, and with them every address)
+  auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
+  const uint32_t bt = scalar(it / p.blocks), blk = it - bt * p.blocks;
+  const uint32_t bh = scalar(bt / p.nQ), t = bt - bh * p.nQ;
+  const uint32_t b = scalar(bh / p.Hkv), h = bh - b * p.Hkv;
   const int K = p.topk;
 
   // ---- the list: lane s holds entry s.  Groups before the first list take the weights of
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   }
   const bool named = j >= 0 && j < p.C;
   j = named ? j : 0;
-  const int length = named ? min(p.tokens[(int64_t)b * p.C + j], kS) : 0;
+  const int length = named ? max(min(p.tokens[(int64_t)b * p.C + j], kS), 0) : 0;
   const int64_t slot0 = (int64_t)bh * p.C;
   const float kscale = named ? p.ks[slot0 + j] : 0.f;
   float vscale = named ? p.vs[slot0 + j] : 0.f;
@@ -201,6 +205,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   // this wave's entries: those whose rank among the valid ones is wave (mod nw)
   const uint64_t all = __ballot(valid && has_list);
   const uint32_t count = __popcll(all);
+  const int entry = (j << 7) | length;  // (one register for both: C <= 2^18)
   uint32_t mine = (uint32_t)__ballot(valid && has_list && ((uint32_t)lanes_below(all) & (nw - 1)) == wave);
 
   const uint32_t nrows = min((uint32_t)QB, p.M - m0);
@@ -215,14 +220,26 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
                                     : 16 * (col >> 2) + (col & 3);
   const uint32_t lane_off = lane_row * kD + 16 * g;
-  auto load_tile = [&](u32x4* x, const uint8_t* base, int slot) {
-    const uint8_t* tile = base + (slot0 + slot) * kTileBytes;
+  // (`there` false: no memory is read.  The loads are issued either way, so that what is in
+  // flight at a wait is known and a wait for one tile does not wait for the next)
+  auto load_tile = [&](u32x4* x, const uint8_t* base, int slot, bool there) {
+    const __amdgpu_buffer_rsrc_t tile = range_rsrc(
+        reinterpret_cast<const char*>(base) + (slot0 + slot) * kTileBytes, there ? kTileBytes : 0);
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
       for (int y = 0; y < NX; ++y)
-        x[a * NX + y] =
-            *reinterpret_cast<const u32x4*>(tile + lane_off + (W == 32 ? 32 : 4) * a * kD + 16 * NG * y);
+        x[a * NX + y] = __builtin_amdgcn_raw_buffer_load_b128(
+            tile, lane_off, (W == 32 ? 32 : 4) * a * kD + 16 * NG * y, 0);
+  };
+
+  // a lane's values of tokens behind the first len set to x (value u is token 32 (u / 16) + 16 g
+  // + u % 16, W = 32, or 16 g + u, W = 16); opaque: compared where it happens, in the rare branch
+  auto cut = [&](float* v, int len, float x) {
+    const int left = opaque(len - 16 * g);
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      if ((W == 32 ? 32 * (u / 16) + u % 16 : u) >= left) v[u] = x;
   };
 
   Acc o[NC][NA];
@@ -233,15 +250,15 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
 
   u32x4 kr[NA * NX], vr[NA * NX];
   if (mine != 0) {
-    const int jn = __builtin_amdgcn_readlane(j, __builtin_ctz(mine));
-    load_tile(kr, p.k, jn);
-    load_tile(vr, p.v, jn);
+    const int jn = __builtin_amdgcn_readlane(entry, __builtin_ctz(mine)) >> 7;
+    load_tile(kr, p.k, jn, true);
+    load_tile(vr, p.v, jn, true);
   }
   while (mine != 0) {
     const int s = __builtin_ctz(mine);
     mine &= mine - 1;
-    const int jn = mine != 0 ? __builtin_amdgcn_readlane(j, __builtin_ctz(mine)) : 0;
-    const int len = __builtin_amdgcn_readlane(length, s);
+    const int jn = mine != 0 ? __builtin_amdgcn_readlane(entry, __builtin_ctz(mine)) >> 7 : 0;
+    const int len = __builtin_amdgcn_readlane(entry, s) & 127;
     const float sc = p.scale * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kscale), s));
     const float cf = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(coef), s));
 
@@ -261,21 +278,16 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
           for (int e = 0; e < QP; ++e) st[c][a] = mma(f, qf[c][i][e], st[c][a]);
       }
     }
-    if (mine != 0) load_tile(kr, p.k, jn);
+    load_tile(kr, p.k, jn, mine != 0);
 
-    // softmax over the chunk's tokens; value u of a lane is token 32 (u / 16) + 16 g + u % 16
-    // (W = 32) or 16 g + u (W = 16)
+    // softmax over the chunk's tokens
     f16x8 pf[NC][NK][PP];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       float v[NV];
 #pragma unroll
       for (int u = 0; u < NV; ++u) v[u] = st[c][u / NR][u % NR];
-      if (len < kS) {
-#pragma unroll
-        for (int u = 0; u < NV; ++u)
-          if ((W == 32 ? 32 * (u / 16) + u % 16 : u) + 16 * g >= len) v[u] = -INFINITY;
-      }
+      if (len < kS) cut(v, len, -INFINITY);
       float mx = fmaxf(fmaxf(v[0], v[1]), v[2]), mx2 = fmaxf(fmaxf(v[3], v[4]), v[5]);
 #pragma unroll
       for (int u = 6; u + 3 < NV; u += 4) {
@@ -292,11 +304,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
       if (p.off_by_one) mx = fmaxf(mx, 0.f);
 #pragma unroll
       for (int u = 0; u < NV; ++u) v[u] = __builtin_amdgcn_exp2f(fmaf(v[u], sc, -mx));
-      if (len < kS) {  // (a scale of zero times -inf)
-#pragma unroll
-        for (int u = 0; u < NV; ++u)
-          if ((W == 32 ? 32 * (u / 16) + u % 16 : u) + 16 * g >= len) v[u] = 0.f;
-      }
+      if (len < kS) cut(v, len, 0.f);  // (a scale of zero times -inf)
       float sum = v[0], sum2 = v[1];
 #pragma unroll
       for (int u = 2; u < NV; u += 2) {
@@ -329,11 +337,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
 
     // O^T += M^T P^T (numbers behind the chunk's last token are cleared: a masked NaN stays out)
     if (len < kS) {
+      const int here = opaque(len - 16 * g);
 #pragma unroll
       for (int y = 0; y < NX; ++y)
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          const int left = len - (16 * (g + NG * y) + 4 * d);
+          const int left = here - (16 * NG * y + 4 * d);
           const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 #pragma unroll
           for (int a = 0; a < NA; ++a) vr[a * NX + y][d] &= keep;
@@ -350,7 +359,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
 #pragma unroll
           for (int e = 0; e < PP; ++e) o[c][a] = mma(f, pf[c][i][e], o[c][a]);
       }
-    if (mine != 0) load_tile(vr, p.v, jn);
+    load_tile(vr, p.v, jn, mine != 0);
   }
 
   // ---- output: value u of a lane is column 32 (u / 16) + 16 g + u % 16 (W = 32) or 16 g + u

@@ -14,11 +14,6 @@ constexpr int kScanWaves = kScanThreads / 64;
 static_assert(kScanWaves == kScanListWaves, "the merge's list mapping assumes four scan waves");
 constexpr int kScanBatch = 8;  // column blocks per lane in one batch of loads
 
-// Buffer descriptor over `bytes` bytes from `base` (wave-uniform): reads at
-// offsets past the end return zero and touch no memory.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_rsrc(const char* base, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00020000);
-}
 constexpr int kLoadNonTemporal = 2;  // cache policy: streamed once
 
 // Partial dot product of one lane's 8 elements of a key column block with the

@@ -74,6 +74,12 @@ __device__ __forceinline__ int opaque(int x) {
   return x;
 }
 
+// Buffer descriptor over `bytes` bytes from `base` (wave-uniform): reads at
+// offsets past the end return zero and touch no memory.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_rsrc(const char* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00020000);
+}
+
 // Number of set bits of a wave-wide mask below this lane (v_mbcnt: no lane mask
 // is formed or kept in registers).
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
