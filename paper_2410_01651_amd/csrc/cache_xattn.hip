@@ -111,6 +111,17 @@ __device__ __forceinline__ f16x8 to_f16(uint32_t x, uint32_t y) {
   }
 }
 
+__device__ __forceinline__ void store8(__bf16* p, const float* x) {
+  bf16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (__bf16)x[e];
+  *reinterpret_cast<bf16x8*>(p) = r;
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  reinterpret_cast<f32x4*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
+  reinterpret_cast<f32x4*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+}
+
 // T: type of the queries; W: MFMA tile; NC: column blocks of W query rows.
 template <typename T, bool I8, int W, int NC>
 __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnParams p) {
@@ -139,6 +150,24 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   const uint32_t b = scalar(bh / p.Hkv), h = bh - b * p.Hkv;
   const int K = p.topk;
 
+  // piece (a, x) of a tile: row tile_row(a) = the token (column) of this lane's operand row,
+  // bytes 16 (g + NG x) ..
+  const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
+                                    : 16 * (col >> 2) + (col & 3);
+  const uint32_t lane_off = lane_row * kD + 16 * g;
+  // (`there` false: no memory is read.  The loads are issued either way, so that what is in
+  // flight at a wait is known and a wait for one tile does not wait for the next)
+  auto load_tile = [&](u32x4* x, const uint8_t* base, int slot, bool there) {
+    const __amdgpu_buffer_rsrc_t tile = range_rsrc(
+        reinterpret_cast<const char*>(base) + ((int64_t)bh * p.C + slot) * kTileBytes, there ? kTileBytes : 0);
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+        x[a * NX + y] = __builtin_amdgcn_raw_buffer_load_b128(
+            tile, lane_off, (W == 32 ? 32 : 4) * a * kD + 16 * NG * y, 0);
+  };
+
   // ---- the list: lane s holds entry s.  Groups before the first list take the weights of
   // the last one, which feeds no group.
   const bool has_list = (int)t >= p.lag;
@@ -147,28 +176,45 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   int j = -1;
   float sv = -INFINITY;
   if (lane < K) {
-    j = p.idx[row * K + lane];
-    sv = p.sel[row * K + lane];
+    j = reinterpret_cast<const int32_t*>(uniform_addr(p.idx + row * K))[lane];
+    sv = reinterpret_cast<const float*>(uniform_addr(p.sel + row * K))[lane];
   }
   const bool named = j >= 0 && j < p.C;
   j = named ? j : 0;
-  const int length = named ? max(min(p.tokens[(int64_t)b * p.C + j], kS), 0) : 0;
   const int64_t slot0 = (int64_t)bh * p.C;
-  const float kscale = named ? p.ks[slot0 + j] : 0.f;
-  float vscale = named ? p.vs[slot0 + j] : 0.f;
+  int length = 0;
+  float kscale = 0.f, vscale = 0.f;
+  if (named) {
+    length = reinterpret_cast<const int32_t*>(uniform_addr(p.tokens + (int64_t)b * p.C))[(uint32_t)j];
+    kscale = reinterpret_cast<const float*>(uniform_addr(p.ks + slot0))[(uint32_t)j];
+    vscale = reinterpret_cast<const float*>(uniform_addr(p.vs + slot0))[(uint32_t)j];
+  }
+
+  // The first tiles that the list names for this wave are asked for at once, beside their lengths
+  // and scales: it is nearly always so that they are in use.
+  auto share = [&](uint64_t entries) {  // this wave's: those whose rank is its number (mod nw)
+    return (uint32_t)(entries & __ballot(((uint32_t)lanes_below(entries) & (nw - 1)) == wave));
+  };
+  const uint32_t guess = has_list ? share(__ballot(named)) : 0;
+  const int first = guess != 0 ? __builtin_amdgcn_readlane(j, __builtin_ctz(guess)) : 0;
+  u32x4 kr[NA * NX], vr[NA * NX];
+  load_tile(kr, p.k, first, guess != 0);
+  load_tile(vr, p.v, first, guess != 0);
 
   // ---- the queries: lane (g, c) takes columns 16 (g + NG x) .. of row c, x < NX
   const uint32_t m0 = blk * QB;
   const bool flat = p.G == 1 || p.nQ == 1;  // a group's rows are consecutive
-  const int64_t row0 = ((int64_t)(b * p.H + h * p.G) * p.nQ + t) * p.rows;
-  auto q_row = [&](uint32_t m) -> int64_t {
-    return row0 + (flat ? m : (int64_t)(m / p.rows) * p.nQ * p.rows + m % p.rows);
+  const int64_t row0 = ((int64_t)(b * p.H + h * p.G) * p.nQ + t) * p.rows + (flat ? m0 : 0);
+  auto ahead = [&](uint32_t m) -> int64_t {  // of the item's row m, from row0
+    if (flat) return m;
+    m += m0;
+    return (int64_t)(m / p.rows) * p.nQ * p.rows + m % p.rows;
   };
   bf16x8 qf[NC][NK][QP];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const uint32_t m = min(m0 + c * W + col, p.M - 1);
-    const T* qr = reinterpret_cast<const T*>(p.q) + q_row(m) * kD;
+    const uint32_t m = min(uint32_t(c * W + col), p.M - 1 - m0);
+    const T* qr = reinterpret_cast<const T*>(uniform_addr(reinterpret_cast<const T*>(p.q) + row0 * kD)) + ahead(m) * kD;
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
       const T* src = qr + 16 * (g + NG * (s >> 1)) + 8 * (s & 1);
@@ -193,6 +239,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   }
 
   // ---- fusion weights (Eq. 2)
+  length = max(min(length, kS), 0);
   const bool valid = length > 0;
   vscale = valid ? vscale : 0.f;  // (a free slot's scale may be anything)
   const float top = max64(valid ? sv : -INFINITY);
@@ -202,11 +249,10 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   if (p.w && wave == 0 && blk == 0 && (p.Hr != 1 || h == 0) && lane < K) p.w[row * K + lane] = wl;
   const float vmax = max64(vscale);
   const float coef = vmax > 0.f ? wl * (vscale / vmax) * 0x1p15f : wl * vscale;
-  // this wave's entries: those whose rank among the valid ones is wave (mod nw)
   const uint64_t all = __ballot(valid && has_list);
   const uint32_t count = __popcll(all);
+  uint32_t mine = share(all);
   const int entry = (j << 7) | length;  // (one register for both: C <= 2^18)
-  uint32_t mine = (uint32_t)__ballot(valid && has_list && ((uint32_t)lanes_below(all) & (nw - 1)) == wave);
 
   const uint32_t nrows = min((uint32_t)QB, p.M - m0);
   float* const lse_s = smem;  // [row][entry]
@@ -214,24 +260,6 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
     for (uint32_t e = threadIdx.x; e < nrows * K; e += blockDim.x) lse_s[e] = -INFINITY;
     __syncthreads();
   }
-
-  // piece (a, x) of a tile: row tile_row(a) = the token (column) of this lane's operand row,
-  // bytes 16 (g + NG x) ..
-  const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
-                                    : 16 * (col >> 2) + (col & 3);
-  const uint32_t lane_off = lane_row * kD + 16 * g;
-  // (`there` false: no memory is read.  The loads are issued either way, so that what is in
-  // flight at a wait is known and a wait for one tile does not wait for the next)
-  auto load_tile = [&](u32x4* x, const uint8_t* base, int slot, bool there) {
-    const __amdgpu_buffer_rsrc_t tile = range_rsrc(
-        reinterpret_cast<const char*>(base) + (slot0 + slot) * kTileBytes, there ? kTileBytes : 0);
-#pragma unroll
-    for (int a = 0; a < NA; ++a)
-#pragma unroll
-      for (int y = 0; y < NX; ++y)
-        x[a * NX + y] = __builtin_amdgcn_raw_buffer_load_b128(
-            tile, lane_off, (W == 32 ? 32 : 4) * a * kD + 16 * NG * y, 0);
-  };
 
   // a lane's values of tokens behind the first len set to x (value u is token 32 (u / 16) + 16 g
   // + u % 16, W = 32, or 16 g + u, W = 16); opaque: compared where it happens, in the rare branch
@@ -248,11 +276,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
 #pragma unroll
     for (int a = 0; a < NA; ++a) o[c][a] = Acc{};
 
-  u32x4 kr[NA * NX], vr[NA * NX];
   if (mine != 0) {
     const int jn = __builtin_amdgcn_readlane(entry, __builtin_ctz(mine)) >> 7;
-    load_tile(kr, p.k, jn, true);
-    load_tile(vr, p.v, jn, true);
+    if (jn != first) {
+      load_tile(kr, p.k, jn, true);
+      load_tile(vr, p.v, jn, true);
+    }
   }
   while (mine != 0) {
     const int s = __builtin_ctz(mine);
@@ -364,17 +393,19 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
 
   // ---- output: value u of a lane is column 32 (u / 16) + 16 g + u % 16 (W = 32) or 16 g + u
   const float osc = vmax > 0.f ? vmax * 0x1p-15f : 1.f;
+  T* const out0 = reinterpret_cast<T*>(uniform_addr(reinterpret_cast<T*>(p.out) + row0 * kD));
   if (nw == 1) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const uint32_t m = c * W + col;
       if (m >= nrows) continue;
-      T* dst = reinterpret_cast<T*>(p.out) + q_row(m0 + m) * kD + 16 * g;
+      T* dst = out0 + ahead(m) * kD + 16 * g;
 #pragma unroll
-      for (int u = 0; u < NV; u += 4) {
-        const Acc& a = o[c][u / NR];
-        store4(dst + (u / 16) * 32 + u % 16, a[u % NR] * osc, a[u % NR + 1] * osc, a[u % NR + 2] * osc,
-               a[u % NR + 3] * osc);
+      for (int u = 0; u < NV; u += 8) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = o[c][(u + e) / NR][(u + e) % NR] * osc;
+        store8(dst + (u / 16) * 32 + u % 16, x);
       }
     }
     if (p.lse) __syncthreads();
@@ -403,14 +434,14 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
       f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
       for (uint32_t y = 0; y < waves; ++y)
         acc += *reinterpret_cast<const f32x4*>(part + (y * nrows + m) * kD + 4 * (x ^ (m & 15)));
-      store4(reinterpret_cast<T*>(p.out) + q_row(m0 + m) * kD + 4 * x, acc[0] * osc, acc[1] * osc, acc[2] * osc,
-             acc[3] * osc);
+      store4(out0 + ahead(m) * kD + 4 * x, acc[0] * osc, acc[1] * osc, acc[2] * osc, acc[3] * osc);
     }
   }
   if (p.lse) {
+    float* const dst = reinterpret_cast<float*>(uniform_addr(p.lse + row0 * K));
     for (uint32_t e = threadIdx.x; e < nrows * K; e += blockDim.x) {
-      const uint32_t m = e / K;
-      p.lse[q_row(m0 + m) * K + (e - m * K)] = lse_s[e];
+      const uint32_t m = flat ? 0 : e / K;
+      dst[flat ? (int64_t)e : ahead(m) * K + (e - m * K)] = lse_s[e];
     }
   }
 }
