@@ -493,72 +493,84 @@ def cache_workspace(c: Cache, op: int, n: int = 0):
     return _torch().empty(max(size, 1), dtype=_torch().uint8, device=c.device), size
 
 
-def _on(c: Cache, stream):
-    """Context in which a cache's call allocates and launches: its device (and the given stream)."""
-    if stream is not None:
-        return _torch().cuda.stream(stream)
-    return _torch().cuda.device(c.index)
+class _At:
+    """Context in which a cache's call allocates and launches, with the stream's handle as its
+    value: the given stream, or the current one of the cache's device, which is made the current
+    device if it is not."""
+
+    def __init__(self, c: Cache, stream):
+        cuda = _torch().cuda
+        self.ctx = None
+        if stream is not None:
+            if stream.device != c.device:
+                raise ValueError(f"the stream is on {stream.device}, the cache on {c.device}")
+            self.ctx, self.raw = cuda.stream(stream), stream.cuda_stream
+        else:
+            if cuda.current_device() != c.index:
+                self.ctx = cuda.device(c.index)
+            self.raw = _torch()._C._cuda_getCurrentRawStream(c.index)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return self.raw
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
 
 
 def _cache_ptr(c: Cache, t, name, dtype, shape):
+    """The address of a tensor of a cache's call (one expression where all is well: these checks are
+    a large part of what a call of a few microseconds costs)."""
     if t is None:
         return None
+    if t.get_device() == c.index and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     if t.device != c.device:
         raise ValueError(f"{name} must be on the cache's device {c.device}, got {t.device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
-
-
-def _cache_stream(c: Cache, stream):
-    if stream is None:
-        return _torch().cuda.current_stream(c.index).cuda_stream
-    if stream.device != c.device:
-        raise ValueError(f"the stream is on {stream.device}, the cache on {c.device}")
-    return stream.cuda_stream
+    raise ValueError(f"{name} must be contiguous")
 
 
 def cache_store(c: Cache, k, v, lmk, slots, lengths=None, stream=None):
     """gca_cache_store: chunks of k, v [B, Hkv, n * 64, 64] (and their landmark keys lmk
     [B, Hr, n, D], or None) into slots [B, n]; lengths [B]: new tokens of each sequence."""
-    torch = _torch()
+    i32 = _torch().int32
     s = c.struct
     if slots.dim() != 2:
         raise ValueError("slots must have shape (B, n)")
-    n = slots.shape[1]
-    kv = (s.B, s.Hkv, n * 64, 64)
-    args = (_cache_ptr(c, k, "k", c.elem, kv), _cache_ptr(c, v, "v", c.elem, kv),
-            _cache_ptr(c, lmk, "lmk", c.elem, (s.B, s.Hr, n, s.D)), _cache_ptr(c, slots, "slots", torch.int32, (s.B, n)),
-            _cache_ptr(c, lengths, "lengths", torch.int32, (s.B,)))
-    st = _cache_stream(c, stream)
-    with _on(c, stream):
-        _check(lib().gca_cache_store(c.ref, *args, n, st))
+    B, n = s.B, slots.shape[1]
+    kv = (B, s.Hkv, n * 64, 64)
+    with _At(c, stream) as st:
+        _check(lib().gca_cache_store(c.ref, _cache_ptr(c, k, "k", c.elem, kv), _cache_ptr(c, v, "v", c.elem, kv),
+                                     _cache_ptr(c, lmk, "lmk", c.elem, (B, s.Hr, n, s.D)),
+                                     _cache_ptr(c, slots, "slots", i32, (B, n)),
+                                     _cache_ptr(c, lengths, "lengths", i32, (B,)), n, st))
 
 
 def cache_select(c: Cache, lmk_q, idx=None, sel=None, w=None, want_w=True, ws=None, stream=None):
     """gca_cache_select: the best slots in use for landmark queries lmk_q [B, Hr, 1, D];
     returns idx, sel, w [B, Hr, 1, topk]."""
     torch = _torch()
+    i32, f32 = torch.int32, torch.float32
     s = c.struct
     rows = (s.B, s.Hr, 1, s.topk)
     qp = _cache_ptr(c, lmk_q, "lmk_q", c.elem, (s.B, s.Hr, 1, s.D))
-    st = _cache_stream(c, stream)
-    with _on(c, stream):
+    with _At(c, stream) as st:
         if idx is None:
-            idx = torch.empty(rows, dtype=torch.int32, device=c.device)
+            idx = torch.empty(rows, dtype=i32, device=c.device)
         if sel is None:
-            sel = torch.empty(rows, dtype=torch.float32, device=c.device)
+            sel = torch.empty(rows, dtype=f32, device=c.device)
         if w is None and want_w:
-            w = torch.empty(rows, dtype=torch.float32, device=c.device)
+            w = torch.empty_like(sel)
         if ws is None:
             ws = cache_workspace(c, CACHE_SELECT)[0]
-        _check(lib().gca_cache_select(c.ref, qp, _cache_ptr(c, idx, "idx", torch.int32, rows),
-                                      _cache_ptr(c, sel, "sel", torch.float32, rows),
-                                      _cache_ptr(c, w, "w", torch.float32, rows),
+        _check(lib().gca_cache_select(c.ref, qp, _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, sel, "sel", f32, rows),
+                                      _cache_ptr(c, w, "w", f32, rows),
                                       _cache_ptr(c, ws, "workspace", torch.uint8, ws.shape), ws.numel(), st))
     return idx, sel, w
 
@@ -568,26 +580,26 @@ def cache_xattn(c: Cache, q, idx, sel, out=None, lse=None, w=None, want_lse=True
     """gca_cache_xattn: query rows q [B, H, nQ * rows, 64] against the chunks that their group's
     list idx, sel [B, Hr, nQ, topk] names (causal: the list before); returns out, lse, w."""
     torch = _torch()
+    i32, f32 = torch.int32, torch.float32
     s = c.struct
     if q.dim() != 4 or idx.dim() != 4:
         raise ValueError("q must have shape (B, H, nQ * rows, 64) and idx (B, Hr, nQ, topk)")
-    nQ, Lq = idx.shape[2], q.shape[2]
+    nQ, Lq, B, H, K = idx.shape[2], q.shape[2], s.B, s.H, s.topk
     if nQ < 1 or Lq < 1 or Lq % nQ:
         raise ValueError(f"q's {Lq} rows are not a positive multiple of idx's {nQ} lists")
-    qs, rows, ls = (s.B, s.H, Lq, 64), (s.B, s.Hr, nQ, s.topk), (s.B, s.H, Lq, s.topk)
-    args = (_cache_ptr(c, q, "q", c.elem, qs), _cache_ptr(c, idx, "idx", torch.int32, rows),
-            _cache_ptr(c, sel, "sel", torch.float32, rows))
-    st = _cache_stream(c, stream)
-    with _on(c, stream):
+    qs, rows, ls = (B, H, Lq, 64), (B, s.Hr, nQ, K), (B, H, Lq, K)
+    qp = _cache_ptr(c, q, "q", c.elem, qs)
+    ip, sp = _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, sel, "sel", f32, rows)
+    with _At(c, stream) as st:
         if out is None:
-            out = torch.empty(qs, dtype=c.elem, device=c.device)
+            out = torch.empty_like(q)
         if lse is None and want_lse:
-            lse = torch.empty(ls, dtype=torch.float32, device=c.device)
+            lse = torch.empty(ls, dtype=f32, device=c.device)
         if w is None and want_w:
-            w = torch.empty(rows, dtype=torch.float32, device=c.device)
-        _check(lib().gca_cache_xattn(c.ref, *args, _cache_ptr(c, out, "out", c.elem, qs),
-                                     _cache_ptr(c, lse, "lse", torch.float32, ls),
-                                     _cache_ptr(c, w, "w", torch.float32, rows), nQ, Lq // nQ, int(bool(causal)), st))
+            w = torch.empty_like(sel)
+        _check(lib().gca_cache_xattn(c.ref, qp, ip, sp, _cache_ptr(c, out, "out", c.elem, qs),
+                                     _cache_ptr(c, lse, "lse", f32, ls), _cache_ptr(c, w, "w", f32, rows), nQ, Lq // nQ,
+                                     int(bool(causal)), st))
     return out, lse, w
 
 
@@ -596,22 +608,23 @@ def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_las
     """gca_cache_evict: adds the weights w of the lists idx [B, Hr, nQ, topk] to the masses and
     returns slots [B, n] for each sequence's next n chunks (want [B]: fewer for some)."""
     torch = _torch()
+    i32, f32 = torch.int32, torch.float32
     s = c.struct
-    lists = tuple(idx.shape) if idx is not None else None
-    if lists is not None and (len(lists) != 4 or lists[2] < 1):
-        raise ValueError("idx must have shape (B, Hr, nQ, topk)")
-    nQ = lists[2] if lists is not None else 0
-    rows = (s.B, s.Hr, nQ, s.topk)
-    args = (_cache_ptr(c, idx, "idx", torch.int32, rows), _cache_ptr(c, w, "w", torch.float32, rows))
-    wp = _cache_ptr(c, want, "want", torch.int32, (s.B,))
-    st = _cache_stream(c, stream)
-    with _on(c, stream):
+    B, nQ = s.B, 0
+    if idx is not None:
+        if idx.dim() != 4 or idx.shape[2] < 1:
+            raise ValueError("idx must have shape (B, Hr, nQ, topk)")
+        nQ = idx.shape[2]
+    rows = (B, s.Hr, nQ, s.topk)
+    ip, wp = _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, w, "w", f32, rows)
+    want_p = _cache_ptr(c, want, "want", i32, (B,))
+    with _At(c, stream) as st:
         if slots is None:
-            slots = torch.empty((s.B, n), dtype=torch.int32, device=c.device)
+            slots = torch.empty((B, n), dtype=i32, device=c.device)
         if ws is None:
             ws = cache_workspace(c, CACHE_EVICT, n)[0]
-        _check(lib().gca_cache_evict(c.ref, *args, nQ, decay, keep_first, keep_last, wp,
-                                     _cache_ptr(c, slots, "slots", torch.int32, (s.B, n)) if n else None, n,
+        _check(lib().gca_cache_evict(c.ref, ip, wp, nQ, decay, keep_first, keep_last, want_p,
+                                     _cache_ptr(c, slots, "slots", i32, (B, n)) if n else None, n,
                                      _cache_ptr(c, ws, "workspace", torch.uint8, ws.shape), ws.numel(), st))
     return slots
 
