@@ -1025,8 +1025,32 @@ __device__ void merge_lists(const float* __restrict__ ls, const int* __restrict_
   const int64_t l_lo = wave * share, l_hi = l_lo + share < lists ? l_lo + share : lists;
   TopList<KM> L;
   L.init();
+  if (share * K <= 64) {
+    // few enough lists for one entry per lane: no need to find the lists worth reading first
+    const int l = lane / K;
+    const int64_t off = (l_lo + l) * K + (lane - l * K);
+    float cs = -INFINITY;
+    int cj = kNoChunk;
+    if (l < share && l_lo + l < l_hi) {
+      const int jj = rj[off];
+      if (jj >= 0) {
+        cs = rs[off];
+        cj = jj;
+      }
+    }
+    wave_top_one(cs, cj, K, ms, mj, cnt);
+    merge_wave_results<KM, NW>(K, sS, sJ, sCnt, ms, mj, cnt);
+    return;
+  }
   // 1. the best k of the share's list maxima
-  if (share <= 128 && K <= 32) {
+  if (share <= 64) {
+    const int64_t l = l_lo + lane;
+    const bool ok = l < l_hi;
+    const int64_t lc = ok ? l : 0;
+    const float v = rs[lc * K];
+    const int j = rj[lc * K];
+    wave_top_one(ok && j >= 0 ? v : -INFINITY, ok && j >= 0 ? j : kNoChunk, K, ms, mj, cnt);
+  } else if (share <= 128 && K <= 32) {
     uint64_t c[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
