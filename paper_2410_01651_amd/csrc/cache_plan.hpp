@@ -9,10 +9,13 @@ namespace gca {
 
 constexpr int64_t kMaxCapacity = 262144;
 
-// Eviction: slots per workgroup of the pass over the masses.  A cache of more slots takes a
-// second launch that chooses among every tile's candidates.
-constexpr int kEvictTile = 8192;
-inline int64_t evict_tiles(const gca_cache& c) { return (c.capacity + kEvictTile - 1) / kEvictTile; }
+// Eviction: one workgroup per sequence for up to kEvictWhole slots; a cache of more is cut into
+// tiles, and a second launch chooses among every tile's candidates.
+constexpr int kEvictWhole = 8192;
+constexpr int kEvictTile = 2048;
+inline int64_t evict_tiles(const gca_cache& c) {
+  return c.capacity <= kEvictWhole ? 1 : (c.capacity + kEvictTile - 1) / kEvictTile;
+}
 // Candidates per tile: enough for the tile to give all n.
 inline int64_t evict_per_tile(int64_t n) { return n < kEvictTile ? n : kEvictTile; }
 inline size_t evict_workspace(const gca_cache& c, int64_t n) {
