@@ -19,7 +19,8 @@ static_assert(sizeof(gca_cache) == 136 && offsetof(gca_cache, capacity) == 24 &&
                   offsetof(gca_cache, k) == 64 && offsetof(gca_cache, next) == 128,
               "gca_cache layout");
 
-constexpr int64_t kMaxItems = int64_t(1) << 26;  // one wave each: a launch holds below 2^32 threads
+// one wave each: a launch holds below 2^32 threads, its workgroups rounded up to a multiple of 8
+constexpr int64_t kMaxItems = (int64_t(1) << 26) - 8;
 
 gca_status check_cache(const gca_cache* c) {
   if (!c) return fail(GCA_ERR_INVALID, "cache pointer is NULL");

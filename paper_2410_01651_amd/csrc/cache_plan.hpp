@@ -41,8 +41,7 @@ inline Shape select_shape(const gca_cache& c) {
   return s;
 }
 
-// Query rows of one cached head's group and the work items they make: blocks of up to 64
-// rows (32 in fp32, 16 where there are no more).
+// Work items of the attention: blocks of 16, 32 or 64 query rows of a group and cached head.
 int64_t xattn_items(const gca_cache& c, int64_t nQ, int64_t rows);
 
 hipError_t launch_cache_store(const gca_cache& c, const void* k, const void* v, const void* lmk, const int32_t* slots,

@@ -53,7 +53,7 @@ struct XattnParams {
   uint32_t part;  // bytes of LDS before the partial outputs
   int topk, lag, off_by_one, C;
   float scale;  // |attn_scale| log2 e
-  int negate;   // attn_scale < 0: the queries' signs are turned
+  uint32_t negate;  // the sign bits of one query entry (fp32) or two, if attn_scale < 0
 };
 
 __device__ __forceinline__ f32x16 mma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
@@ -220,13 +220,13 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
       const T* src = qr + 16 * (g + NG * (s >> 1)) + 8 * (s & 1);
       if constexpr (kB16) {
         u32x4 x = *reinterpret_cast<const u32x4*>(src);
-        if (p.negate) x ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+        x ^= u32x4{p.negate, p.negate, p.negate, p.negate};
         qf[c][s][0] = __builtin_bit_cast(bf16x8, x);
       } else {
 #pragma unroll
         for (int m8 = 0; m8 < 8; ++m8) {
           float x = src[m8];
-          if (p.negate) x = -x;
+          x = __uint_as_float(__float_as_uint(x) ^ p.negate);
 #pragma unroll
           for (int e = 0; e < QP; ++e) {
             const __bf16 part = (__bf16)x;
@@ -446,24 +446,29 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   }
 }
 
-// Rows per item: 16 where the group has no more; 32; 64 in bf16 (both halves share a tile's
-// unpacking; fp32 queries in three terms leave no registers for it).
-int rows_per_item(const gca_cache& c, int64_t M) {
+// Rows per item: 16 where a group has no more; else 32, or in bf16 64, which unpacks a tile for
+// both halves but has two waves per SIMD where 32 has three (fp32 queries in three terms leave no
+// registers for it).  64 where such items give every SIMD two waves and waste no half: groups of 64
+// rows, 8 entries each, 32 / 64 rows per item, us: 64 groups 6.7 / 8.9, 512 12.4 / 13.4, 1,024 18.3 /
+// 20.8, 2,048 30.7 / 29.7, 4,096 60.8 / 58.2, 8,192 127 / 116; of 130 rows, 768 groups 27.8 / 35.3.
+int rows_per_item(const gca_cache& c, int64_t nQ, int64_t M) {
   if (M <= 16) return 16;
-  return M <= 32 || c.dtype != GCA_BF16 ? 32 : 64;
+  const int64_t halves = (M + 31) / 32, groups = (int64_t)c.B * c.Hkv * nQ;
+  const bool whole = halves % 2 == 0 || halves >= 8;
+  return c.dtype == GCA_BF16 && whole && groups * (halves / 2) >= 8 * device_cus() ? 64 : 32;
 }
 
 }  // namespace
 
 int64_t xattn_items(const gca_cache& c, int64_t nQ, int64_t rows) {
-  const int64_t M = (int64_t)(c.H / c.Hkv) * rows, per = rows_per_item(c, M);
+  const int64_t M = (int64_t)(c.H / c.Hkv) * rows, per = rows_per_item(c, nQ, M);
   return (int64_t)c.B * c.Hkv * nQ * ((M + per - 1) / per);
 }
 
 hipError_t launch_cache_xattn(const gca_cache& c, const void* q, const int32_t* idx, const float* sel, void* out,
                               float* lse, float* w, int64_t nQ, int64_t rows, int lag, hipStream_t stream) {
   const int64_t M = (int64_t)(c.H / c.Hkv) * rows;
-  const int qb = rows_per_item(c, M);
+  const int qb = rows_per_item(c, nQ, M);
   XattnParams p;
   p.k = static_cast<const uint8_t*>(c.k);
   p.v = static_cast<const uint8_t*>(c.v);
@@ -490,7 +495,7 @@ hipError_t launch_cache_xattn(const gca_cache& c, const void* q, const int32_t* 
   p.off_by_one = c.off_by_one;
   p.C = (int)c.capacity;
   p.scale = fabsf(c.attn_scale) * kLog2e;
-  p.negate = c.attn_scale < 0.f;
+  p.negate = c.attn_scale < 0.f ? (c.dtype == GCA_BF16 ? 0x80008000u : 0x80000000u) : 0u;
   const int rb = (int)(M < qb ? M : qb);
   p.part = lse ? (uint32_t)((rb * c.topk * sizeof(float) + 15) & ~size_t(15)) : 0u;
   // Waves per item: enough to fill the chip's eight waves per CU, no more than the list has

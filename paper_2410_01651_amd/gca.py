@@ -435,6 +435,7 @@ class Cache:
         self.ref = ctypes.byref(struct)
         self.device = device
         self.index = index    # the device's ordinal
+        self.dims = struct.B, struct.H, struct.Hkv, struct.Hr, struct.D, struct.topk
         self.elem = _torch().bfloat16 if struct.dtype == GCA_BF16 else _torch().float32
         for name in self.NAMES:
             setattr(self, name, tensors[name])
@@ -540,14 +541,14 @@ def cache_store(c: Cache, k, v, lmk, slots, lengths=None, stream=None):
     """gca_cache_store: chunks of k, v [B, Hkv, n * 64, 64] (and their landmark keys lmk
     [B, Hr, n, D], or None) into slots [B, n]; lengths [B]: new tokens of each sequence."""
     i32 = _torch().int32
-    s = c.struct
+    B, _, Hkv, Hr, D, _ = c.dims
     if slots.dim() != 2:
         raise ValueError("slots must have shape (B, n)")
-    B, n = s.B, slots.shape[1]
-    kv = (B, s.Hkv, n * 64, 64)
+    n = slots.shape[1]
+    kv = (B, Hkv, n * 64, 64)
     with _At(c, stream) as st:
         _check(lib().gca_cache_store(c.ref, _cache_ptr(c, k, "k", c.elem, kv), _cache_ptr(c, v, "v", c.elem, kv),
-                                     _cache_ptr(c, lmk, "lmk", c.elem, (B, s.Hr, n, s.D)),
+                                     _cache_ptr(c, lmk, "lmk", c.elem, (B, Hr, n, D)),
                                      _cache_ptr(c, slots, "slots", i32, (B, n)),
                                      _cache_ptr(c, lengths, "lengths", i32, (B,)), n, st))
 
@@ -557,9 +558,9 @@ def cache_select(c: Cache, lmk_q, idx=None, sel=None, w=None, want_w=True, ws=No
     returns idx, sel, w [B, Hr, 1, topk]."""
     torch = _torch()
     i32, f32 = torch.int32, torch.float32
-    s = c.struct
-    rows = (s.B, s.Hr, 1, s.topk)
-    qp = _cache_ptr(c, lmk_q, "lmk_q", c.elem, (s.B, s.Hr, 1, s.D))
+    B, _, _, Hr, D, K = c.dims
+    rows = (B, Hr, 1, K)
+    qp = _cache_ptr(c, lmk_q, "lmk_q", c.elem, (B, Hr, 1, D))
     with _At(c, stream) as st:
         if idx is None:
             idx = torch.empty(rows, dtype=i32, device=c.device)
@@ -581,13 +582,13 @@ def cache_xattn(c: Cache, q, idx, sel, out=None, lse=None, w=None, want_lse=True
     list idx, sel [B, Hr, nQ, topk] names (causal: the list before); returns out, lse, w."""
     torch = _torch()
     i32, f32 = torch.int32, torch.float32
-    s = c.struct
+    B, H, _, Hr, _, K = c.dims
     if q.dim() != 4 or idx.dim() != 4:
         raise ValueError("q must have shape (B, H, nQ * rows, 64) and idx (B, Hr, nQ, topk)")
-    nQ, Lq, B, H, K = idx.shape[2], q.shape[2], s.B, s.H, s.topk
+    nQ, Lq = idx.shape[2], q.shape[2]
     if nQ < 1 or Lq < 1 or Lq % nQ:
         raise ValueError(f"q's {Lq} rows are not a positive multiple of idx's {nQ} lists")
-    qs, rows, ls = (B, H, Lq, 64), (B, s.Hr, nQ, K), (B, H, Lq, K)
+    qs, rows, ls = (B, H, Lq, 64), (B, Hr, nQ, K), (B, H, Lq, K)
     qp = _cache_ptr(c, q, "q", c.elem, qs)
     ip, sp = _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, sel, "sel", f32, rows)
     with _At(c, stream) as st:
@@ -609,13 +610,13 @@ def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_las
     returns slots [B, n] for each sequence's next n chunks (want [B]: fewer for some)."""
     torch = _torch()
     i32, f32 = torch.int32, torch.float32
-    s = c.struct
-    B, nQ = s.B, 0
+    B, _, _, Hr, _, K = c.dims
+    nQ = 0
     if idx is not None:
         if idx.dim() != 4 or idx.shape[2] < 1:
             raise ValueError("idx must have shape (B, Hr, nQ, topk)")
         nQ = idx.shape[2]
-    rows = (B, s.Hr, nQ, s.topk)
+    rows = (B, Hr, nQ, K)
     ip, wp = _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, w, "w", f32, rows)
     want_p = _cache_ptr(c, want, "want", i32, (B,))
     with _At(c, stream) as st:
