@@ -2,7 +2,13 @@
 // landmark keys with the free slots left out (decode_scan.hpp, MASK), then one workgroup per
 // retrieval row merges the scan's lists into the row's best k and writes them ascending by
 // slot with their fusion weights.  The scan is bound by reading the landmarks once, the merge
-// by its chain of dependent reads.
+// by its chain of dependent steps.
+//
+// The merge's waves each take a share of the lists and keep their best 64 candidates as one
+// sorted 64-bit key per lane.  Candidates that beat the k-th are gathered in LDS until there are
+// 64, sorted and merged in (27 compare-exchange steps).  First come the lists' heads; an entry of
+// the row's k best can only sit in a list whose head is among its share's k best, and as a list is
+// sorted, its next entries are read only while one before them was kept.
 #include "cache_plan.hpp"
 #include "decode_scan.hpp"
 
@@ -10,23 +16,135 @@ namespace gca {
 namespace {
 
 constexpr int kMergeThreads = 512;
+constexpr int kMergeWaves = kMergeThreads / 64;
 
-template <int KM>
+// One step of a bitonic merge, largest first: lane l against l ^ J.
+template <int J>
+__device__ __forceinline__ uint64_t merge_step(uint64_t k) {
+  uint32_t a0, a1, b0, b1;
+  const uint32_t lo = (uint32_t)k, hi = (uint32_t)(k >> 32);
+  if constexpr (J == 32) {
+    pair32(lo, a0, b0);
+    pair32(hi, a1, b1);
+  } else if constexpr (J == 16) {
+    pair16(lo, a0, b0);
+    pair16(hi, a1, b1);
+  } else {
+    a0 = lo;
+    a1 = hi;
+    b0 = J == 8 ? dpp<kDppRor8>(lo) : J == 4 ? swz_xor4(lo) : J == 2 ? dpp<kDppXor2>(lo) : dpp<kDppXor1>(lo);
+    b1 = J == 8 ? dpp<kDppRor8>(hi) : J == 4 ? swz_xor4(hi) : J == 2 ? dpp<kDppXor2>(hi) : dpp<kDppXor1>(hi);
+  }
+  const uint64_t a = (uint64_t)a0 | ((uint64_t)a1 << 32), b = (uint64_t)b0 | ((uint64_t)b1 << 32);
+  return ((a > b) == ((threadIdx.x & J) == 0)) ? a : b;
+}
+
+// A wave's best 64 candidates so far (lane r: the r-th; 0: none) and those waiting to join.
+struct Best {
+  uint64_t key = 0;
+  uint64_t bar = 0;   // the k-th best: only better ones join
+  uint32_t held = 0;
+  uint64_t* buf;      // 128 of this wave's own
+  int K;
+
+  __device__ __forceinline__ Best(uint64_t* b, int k) : buf(b), K(k) {}
+  // the candidates are the lanes' (0: none)
+  __device__ __forceinline__ void start(uint64_t x) {
+    key = wave_sort_desc(x);
+    bar = __shfl(key, K - 1);
+  }
+  // up to 64 waiting candidates join
+  __device__ __forceinline__ void flush() {
+    const int lane = threadIdx.x & 63;
+    wave_lds_order();
+    const uint64_t x = lane < (int)held ? buf[lane] : 0;
+    const uint64_t rest = buf[64 + lane];
+    wave_lds_order();
+    buf[lane] = rest;
+    held = held > 64 ? held - 64 : 0;
+    // descending against ascending: the larger of each pair are the 64 best, in bitonic order
+    const uint64_t up = ~wave_sort_desc(~x);
+    key = key > up ? key : up;
+    key = merge_step<1>(merge_step<2>(merge_step<4>(merge_step<8>(merge_step<16>(merge_step<32>(key))))));
+    bar = __shfl(key, K - 1);
+  }
+  // every lane offers a candidate (0: none)
+  __device__ __forceinline__ void offer(uint64_t x) {
+    const bool in = x > bar;
+    const uint64_t mask = __ballot(in);
+    if (in) buf[held + lanes_below(mask)] = x;
+    held += __popcll(mask);
+    if (held >= 64) flush();
+  }
+  __device__ __forceinline__ void settle() {
+    while (held) flush();
+  }
+};
+
 __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(const float* __restrict__ ls,
                                                                     const int* __restrict__ lj, int64_t lists,
                                                                     int64_t pw, int K, int32_t* __restrict__ idx,
                                                                     float* __restrict__ sel, float* __restrict__ w) {
-  constexpr int NW = kMergeThreads / 64;
-  __shared__ float sS[NW * 32];
-  __shared__ int sJ[NW * 32];
-  __shared__ int sCnt[NW];
-  const int lane = threadIdx.x & 63;
+  __shared__ uint64_t buf[kMergeWaves][128];
+  __shared__ uint64_t result[kMergeWaves][32];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = blockIdx.x;
-  float ms;
-  int mj, cnt;
-  merge_lists<KM, NW>(ls, lj, row, lists, pw, K, sS, sJ, sCnt, ms, mj, cnt);
-  if (threadIdx.x >= 64) return;
-  const bool valid = lane < cnt;
+  const float* rs = ls + row * lists * K;
+  const int* rj = lj + row * lists * K;
+  const int64_t share = (lists + kMergeWaves - 1) / kMergeWaves;
+  const int64_t l_lo = wave * share, l_hi = l_lo + share < lists ? l_lo + share : lists;
+  auto entry = [&](int64_t at) -> uint64_t {
+    const float v = rs[at];
+    const int j = rj[at];
+    return j >= 0 ? pack_key(v, j) : 0;
+  };
+  Best best(buf[wave], K);
+  if (share * K <= 64) {
+    // an entry per lane
+    const int l = lane / K;
+    best.start(l_lo + l < l_hi && l < share ? entry(l_lo * K + lane) : 0);
+  } else {
+    if (share <= 64) {
+      best.start(l_lo + lane < l_hi ? entry((l_lo + lane) * K) : 0);
+    } else {
+      for (int64_t l0 = l_lo; l0 < l_hi; l0 += 64) best.offer(l0 + lane < l_hi ? entry((l0 + lane) * K) : 0);
+      best.settle();
+    }
+    // lane s < K: the list that the s-th best head heads
+    const uint64_t head = lane < K ? best.key : 0;
+    const int list = head != 0 ? (int)scan_list_of(key_chunk(head), pw) : -1;
+    if (K * K <= 64) {
+      const int l = __shfl(list, lane / K);
+      best.start(lane < K * K && l >= 0 ? entry((int64_t)l * K + lane % K) : 0);
+    } else {
+      bool more = list >= 0;
+      for (int r = 1; r < K; r += 4) {
+        uint64_t x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = more && r + u < K ? entry((int64_t)list * K + r + u) : 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) best.offer(x[u]);
+        more = more && x[3] > best.bar;  // (else nothing behind it can join)
+        if (__ballot(more) == 0) break;
+      }
+      best.settle();
+    }
+  }
+  if (lane < K) result[wave][lane] = best.key;
+  __syncthreads();
+  if (wave != 0) return;
+  if (kMergeWaves * K <= 64) {
+    best.start(lane < kMergeWaves * K ? result[lane / K][lane % K] : 0);
+  } else {
+    for (int y = 1; y < kMergeWaves; ++y) best.offer(lane < K ? result[y][lane] : 0);
+    best.settle();
+  }
+
+  const uint64_t key = lane < K ? best.key : 0;
+  const bool valid = key != 0;
+  const int cnt = __popcll(__ballot(valid));
+  const int mj = valid ? key_chunk(key) : kNoChunk;
+  const float ms = valid ? key_score(key) : -INFINITY;
   const int rank = rank_by_chunk(mj, cnt);
   // best first: lane 0 holds the maximum; the valid lanes sit in the lower half
   const float mx = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(ms)));
@@ -35,7 +153,7 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(const float*
   if (lane < K) {
     const int64_t at = row * K + (valid ? rank : lane);
     idx[at] = valid ? mj : -1;
-    sel[at] = valid ? ms : -INFINITY;
+    sel[at] = ms;
     if (w) w[at] = valid ? e / sum : 0.f;
   }
 }
@@ -49,10 +167,8 @@ hipError_t launch_cache_select(const gca_cache& c, const void* lmk_q, int32_t* i
                               : launch_scan<float, false, true>(s, lmk_q, c.lmk, c.tokens, ws, stream);
   if (e != hipSuccess) return e;
   const DecodePlan plan = decode_plan(s);
-  launch_kernel("cache_merge_kernel",
-                s.topk <= 8 ? cache_merge_kernel<8> : s.topk <= 16 ? cache_merge_kernel<16> : cache_merge_kernel<32>,
-                dim3((unsigned)((int64_t)s.B * s.Hr)), dim3(kMergeThreads), 0, stream, decode_list_scores(s, ws),
-                decode_list_chunks(s, ws), plan.lists, plan.pw, s.topk, idx, sel, w);
+  launch_kernel("cache_merge_kernel", cache_merge_kernel, dim3((unsigned)((int64_t)s.B * s.Hr)), dim3(kMergeThreads), 0,
+                stream, decode_list_scores(s, ws), decode_list_chunks(s, ws), plan.lists, plan.pw, s.topk, idx, sel, w);
   return take_launch_error();
 }
 

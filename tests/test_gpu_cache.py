@@ -347,6 +347,9 @@ SELECT = [
     (1, 1, 1, 5000, 32, 64, "fp32", 0.3),
     (1, 1, 1, 70000, 5, 512, "bf16", 0.99),    # more keys than the lanes keep
     (300, 1, 1, 600, 3, 64, "bf16", 0.6),      # one workgroup scans a row
+    (1, 1, 1, 40000, 32, 64, "bf16", 0.9),     # a thousand lists to merge
+    (2, 2, 2, 20000, 16, 64, "fp32", 0.02),    # most of them empty
+    (1, 1, 1, 3000, 17, 128, "bf16", 0.8),
     (2, 1, 1, 200, 4, 8192, "fp32", 0.5),
 ]
 
