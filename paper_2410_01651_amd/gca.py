@@ -417,7 +417,7 @@ def forward_noalloc(p: Problem, lmk_q, lmk_k, q, k, v, out, idx, sel, lse=None, 
 
 class Cache:
     """A bounded 8-bit chunk cache (``gca_cache``): its sizes and its device tensors, which
-    are the program's own and may be read or, between calls, changed:
+    are the program's own and may be read or, between calls, changed in place:
 
     * ``k`` [B, Hkv, C, 64 tokens, 64], ``v`` [B, Hkv, C, 64, 64 tokens]: 8-bit numbers
       (``torch.float8_e4m3fn`` or ``torch.int8``), values transposed per chunk;
@@ -431,12 +431,13 @@ class Cache:
     NAMES = ("k", "v", "k_scale", "v_scale", "lmk", "tokens", "mass", "number", "next")
 
     def __init__(self, struct, tensors, device, index):
+        self.torch = torch = _torch()
         self.struct = struct
         self.ref = ctypes.byref(struct)
         self.device = device
         self.index = index    # the device's ordinal
         self.dims = struct.B, struct.H, struct.Hkv, struct.Hr, struct.D, struct.topk
-        self.elem = _torch().bfloat16 if struct.dtype == GCA_BF16 else _torch().float32
+        self.elem = torch.bfloat16 if struct.dtype == GCA_BF16 else torch.float32
         for name in self.NAMES:
             setattr(self, name, tensors[name])
 
@@ -500,16 +501,16 @@ class _At:
     device if it is not."""
 
     def __init__(self, c: Cache, stream):
-        cuda = _torch().cuda
+        torch = c.torch
         self.ctx = None
-        if stream is not None:
+        if stream is None:
+            if torch.cuda.current_device() != c.index:
+                self.ctx = torch.cuda.device(c.index)
+            self.raw = torch._C._cuda_getCurrentRawStream(c.index)
+        else:
             if stream.device != c.device:
                 raise ValueError(f"the stream is on {stream.device}, the cache on {c.device}")
-            self.ctx, self.raw = cuda.stream(stream), stream.cuda_stream
-        else:
-            if cuda.current_device() != c.index:
-                self.ctx = cuda.device(c.index)
-            self.raw = _torch()._C._cuda_getCurrentRawStream(c.index)
+            self.ctx, self.raw = torch.cuda.stream(stream), stream.cuda_stream
 
     def __enter__(self):
         if self.ctx is not None:
@@ -537,10 +538,16 @@ def _cache_ptr(c: Cache, t, name, dtype, shape):
     raise ValueError(f"{name} must be contiguous")
 
 
+def _new(c: Cache, shape, dtype, like=None):
+    """A new output and its address (nothing to check); `like`: a tensor of its shape and type."""
+    t = c.torch.empty(shape, dtype=dtype, device=c.device) if like is None else c.torch.empty_like(like)
+    return t, t.data_ptr()
+
+
 def cache_store(c: Cache, k, v, lmk, slots, lengths=None, stream=None):
     """gca_cache_store: chunks of k, v [B, Hkv, n * 64, 64] (and their landmark keys lmk
     [B, Hr, n, D], or None) into slots [B, n]; lengths [B]: new tokens of each sequence."""
-    i32 = _torch().int32
+    i32 = c.torch.int32
     B, _, Hkv, Hr, D, _ = c.dims
     if slots.dim() != 2:
         raise ValueError("slots must have shape (B, n)")
@@ -556,23 +563,22 @@ def cache_store(c: Cache, k, v, lmk, slots, lengths=None, stream=None):
 def cache_select(c: Cache, lmk_q, idx=None, sel=None, w=None, want_w=True, ws=None, stream=None):
     """gca_cache_select: the best slots in use for landmark queries lmk_q [B, Hr, 1, D];
     returns idx, sel, w [B, Hr, 1, topk]."""
-    torch = _torch()
-    i32, f32 = torch.int32, torch.float32
+    i32, f32 = c.torch.int32, c.torch.float32
     B, _, _, Hr, D, K = c.dims
     rows = (B, Hr, 1, K)
-    qp = _cache_ptr(c, lmk_q, "lmk_q", c.elem, (B, Hr, 1, D))
+    qp, ip = _cache_ptr(c, lmk_q, "lmk_q", c.elem, (B, Hr, 1, D)), _cache_ptr(c, idx, "idx", i32, rows)
+    sp, wp = _cache_ptr(c, sel, "sel", f32, rows), _cache_ptr(c, w, "w", f32, rows)
     with _At(c, stream) as st:
         if idx is None:
-            idx = torch.empty(rows, dtype=i32, device=c.device)
+            idx, ip = _new(c, rows, i32)
         if sel is None:
-            sel = torch.empty(rows, dtype=f32, device=c.device)
+            sel, sp = _new(c, rows, f32)
         if w is None and want_w:
-            w = torch.empty_like(sel)
+            w, wp = _new(c, rows, f32, sel)
         if ws is None:
             ws = cache_workspace(c, CACHE_SELECT)[0]
-        _check(lib().gca_cache_select(c.ref, qp, _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, sel, "sel", f32, rows),
-                                      _cache_ptr(c, w, "w", f32, rows),
-                                      _cache_ptr(c, ws, "workspace", torch.uint8, ws.shape), ws.numel(), st))
+        _check(lib().gca_cache_select(c.ref, qp, ip, sp, wp, _cache_ptr(c, ws, "workspace", c.torch.uint8, ws.shape),
+                                      ws.numel(), st))
     return idx, sel, w
 
 
@@ -580,8 +586,7 @@ def cache_xattn(c: Cache, q, idx, sel, out=None, lse=None, w=None, want_lse=True
                 stream=None):
     """gca_cache_xattn: query rows q [B, H, nQ * rows, 64] against the chunks that their group's
     list idx, sel [B, Hr, nQ, topk] names (causal: the list before); returns out, lse, w."""
-    torch = _torch()
-    i32, f32 = torch.int32, torch.float32
+    i32, f32 = c.torch.int32, c.torch.float32
     B, H, _, Hr, _, K = c.dims
     if q.dim() != 4 or idx.dim() != 4:
         raise ValueError("q must have shape (B, H, nQ * rows, 64) and idx (B, Hr, nQ, topk)")
@@ -589,18 +594,17 @@ def cache_xattn(c: Cache, q, idx, sel, out=None, lse=None, w=None, want_lse=True
     if nQ < 1 or Lq < 1 or Lq % nQ:
         raise ValueError(f"q's {Lq} rows are not a positive multiple of idx's {nQ} lists")
     qs, rows, ls = (B, H, Lq, 64), (B, Hr, nQ, K), (B, H, Lq, K)
-    qp = _cache_ptr(c, q, "q", c.elem, qs)
-    ip, sp = _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, sel, "sel", f32, rows)
+    qp, ip = _cache_ptr(c, q, "q", c.elem, qs), _cache_ptr(c, idx, "idx", i32, rows)
+    sp, op = _cache_ptr(c, sel, "sel", f32, rows), _cache_ptr(c, out, "out", c.elem, qs)
+    lp, wp = _cache_ptr(c, lse, "lse", f32, ls), _cache_ptr(c, w, "w", f32, rows)
     with _At(c, stream) as st:
         if out is None:
-            out = torch.empty_like(q)
+            out, op = _new(c, qs, c.elem, q)
         if lse is None and want_lse:
-            lse = torch.empty(ls, dtype=f32, device=c.device)
+            lse, lp = _new(c, ls, f32)
         if w is None and want_w:
-            w = torch.empty_like(sel)
-        _check(lib().gca_cache_xattn(c.ref, qp, ip, sp, _cache_ptr(c, out, "out", c.elem, qs),
-                                     _cache_ptr(c, lse, "lse", f32, ls), _cache_ptr(c, w, "w", f32, rows), nQ, Lq // nQ,
-                                     int(bool(causal)), st))
+            w, wp = _new(c, rows, f32, sel)
+        _check(lib().gca_cache_xattn(c.ref, qp, ip, sp, op, lp, wp, nQ, Lq // nQ, int(bool(causal)), st))
     return out, lse, w
 
 
@@ -608,8 +612,7 @@ def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_las
                 stream=None):
     """gca_cache_evict: adds the weights w of the lists idx [B, Hr, nQ, topk] to the masses and
     returns slots [B, n] for each sequence's next n chunks (want [B]: fewer for some)."""
-    torch = _torch()
-    i32, f32 = torch.int32, torch.float32
+    i32, f32 = c.torch.int32, c.torch.float32
     B, _, _, Hr, _, K = c.dims
     nQ = 0
     if idx is not None:
@@ -618,15 +621,14 @@ def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_las
         nQ = idx.shape[2]
     rows = (B, Hr, nQ, K)
     ip, wp = _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, w, "w", f32, rows)
-    want_p = _cache_ptr(c, want, "want", i32, (B,))
+    want_p, sp = _cache_ptr(c, want, "want", i32, (B,)), _cache_ptr(c, slots, "slots", i32, (B, n))
     with _At(c, stream) as st:
         if slots is None:
-            slots = torch.empty((B, n), dtype=i32, device=c.device)
+            slots, sp = _new(c, (B, n), i32)
         if ws is None:
             ws = cache_workspace(c, CACHE_EVICT, n)[0]
-        _check(lib().gca_cache_evict(c.ref, ip, wp, nQ, decay, keep_first, keep_last, want_p,
-                                     _cache_ptr(c, slots, "slots", i32, (B, n)) if n else None, n,
-                                     _cache_ptr(c, ws, "workspace", torch.uint8, ws.shape), ws.numel(), st))
+        _check(lib().gca_cache_evict(c.ref, ip, wp, nQ, decay, keep_first, keep_last, want_p, sp if n else None, n,
+                                     _cache_ptr(c, ws, "workspace", c.torch.uint8, ws.shape), ws.numel(), st))
     return slots
 
 
