@@ -232,7 +232,8 @@ gca_status gca_forward_noalloc(const gca_problem* p, const void* lmk_q, const vo
  * the slots to attend to by landmark, attend to them, and evict the chunks that were
  * attended to least.  All state is the caller's device memory, named in gca_cache; every
  * call reads lengths, slots and counters on the device, so a serving loop needs no
- * synchronisation and can be captured into a HIP graph.
+ * synchronisation and can be captured into a HIP graph.  Calls on one cache are ordered by the
+ * caller (one stream, or events), as are calls that share a workspace.
  *
  * GCA has no positions between chunks (Methodology: retrieved chunks are attended to one
  * by one), so a chunk may sit in any slot; ties between scores go to the lower slot.
@@ -317,7 +318,8 @@ gca_status gca_cache_select(const gca_cache* c, const void* lmk_q, int32_t* idx,
  *                                      (-inf on pads), may be NULL
  *   w   [B, Hr, nQ, topk]       fp32   output: fusion weights of every list, may be NULL
  * Products of q with the cached numbers are exact and summed in fp32; probabilities are
- * rounded to fp16 (fp32 tensors: to two fp16 terms) before they meet the values.
+ * rounded to fp16 (fp32 tensors: to two fp16 terms), and in any case to no less than 2^-40,
+ * before they meet the values.
  * Requires c->k, v, k_scale, v_scale, tokens. */
 gca_status gca_cache_xattn(const gca_cache* c, const void* q, const int32_t* idx, const float* sel, void* out,
                            float* lse, float* w, int64_t nQ, int64_t rows, int32_t lag, hipStream_t stream);

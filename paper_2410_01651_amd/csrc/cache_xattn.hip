@@ -13,7 +13,7 @@
 // Layout.  The products are formed transposed, S^T = N Q^T and O^T = M^T P^T, on MFMA tiles of
 // W x W (W = 32, or 16 for at most 16 rows): lane l = W g + c has query row c as its column.
 // Row m of block a of N is not token W a + m but the token that makes a lane's accumulators
-// consecutive tokens (`tile_row`): W = 32: 32 a + 16 g + (0..15); W = 16: 16 g + (0..15).  They are
+// consecutive tokens (`lane_row`): W = 32: 32 a + 16 g + (0..15); W = 16: 16 g + (0..15).  They are
 // then, rounded, the operand of the second product as they stand, and what a lane needs of M
 // (stored transposed: columns of a chunk's values are rows) are 16 consecutive bytes; so are
 // its columns of N.  A tile is 4 loads of 16 bytes per lane straight from the cache into
@@ -150,13 +150,14 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   const uint32_t b = scalar(bh / p.Hkv), h = bh - b * p.Hkv;
   const int K = p.topk;
 
-  // piece (a, x) of a tile: row tile_row(a) = the token (column) of this lane's operand row,
-  // bytes 16 (g + NG x) ..
+  // piece (a, y) of a tile: its row lane_row + 32 a (W = 32) or + 4 a, the token (column) of this
+  // lane's operand row, bytes 16 (g + NG y) ..
   const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
                                     : 16 * (col >> 2) + (col & 3);
   const uint32_t lane_off = lane_row * kD + 16 * g;
-  // (`there` false: no memory is read.  The loads are issued either way, so that what is in
-  // flight at a wait is known and a wait for one tile does not wait for the next)
+  // (`there` false: nothing is wanted, and the descriptor is empty.  The loads are issued either
+  // way, so that what is in flight at a wait is known and a wait for one tile does not wait for the
+  // next; the address is always that of one of the cache's own tiles.)
   auto load_tile = [&](u32x4* x, const uint8_t* base, int slot, bool there) {
     const __amdgpu_buffer_rsrc_t tile = range_rsrc(
         reinterpret_cast<const char*>(base) + ((int64_t)bh * p.C + slot) * kTileBytes, there ? kTileBytes : 0);

@@ -7,7 +7,11 @@ product with the scale included).  An exponential of such a score is off by that
 amount (twice, once through the maximum) and by 4 u of its own; a normalised weight twice that.
 So a row's output is off by at most 4 x 66 u dot + 64 u (its fp32 sums and the fusion weights)
 plus the rounding of the probabilities (bf16 tensors: 2^-11 for fp16; fp32: 2^-22 for two terms) of
-sum w p |v| (`mag`), and by its own rounding (2^-8 bf16, 2^-24 fp32) of its value."""
+sum w p |v| (`mag`), and by its own rounding (2^-8 bf16, 2^-24 fp32) of its value.  That is so
+for normal fp16 numbers; below 2^-14 fp16 has steps of 2^-24, so a scaled probability (2^15 w p
+times its value scale over the list's largest, nu) is off by up to 2^-25 whatever its size, which
+nu 2^-15 turns into 2^-40 nu of each number's magnitude (`num` = nu sum |number|): it shows only
+in outputs some 1e-12 of the values, where every heavy key's value is nearly zero."""
 
 import numpy as np
 import pytest
@@ -77,6 +81,7 @@ def _check_xattn(c, q, idx, sel, got, rows, lag):
     bf16 = s.dtype == 1
     rel = 4 * 66 * U * ref["dot"] + 64 * U
     bound = (rel[..., None] + (2.0**-11 if bf16 else 2.0**-22)) * ref["mag"] + (2.0**-8 if bf16 else U) * np.abs(ref["out"])
+    bound += 2.0**-40 * ref["num"]
     err = np.abs(host64(out) - ref["out"])
     assert (err <= bound * (1 + 2.0**-7) + 1e-30).all(), float((err / (bound + 1e-300)).max())
     if lse is not None:
@@ -106,6 +111,11 @@ XATTN = [
     (1, 1, 1, 1, 300, 1, 260, 1, 1, "bf16", "e4m3", False, True),   # many lists of one entry
     (3, 2, 2, 2, 30, 9, 90, 40, 0, "bf16", "e4m3", False, True),    # more items than waves
     (1, 1, 1, 1, 5, 4, 1, 1000, 0, "fp32", "e4m3", True, False),    # many row blocks
+    # enough groups for 64 rows per wave: full, a row over half, two heads' rows apart, four blocks
+    (2, 4, 4, 1, 40, 3, 256, 64, 1, "bf16", "e4m3", False, True),
+    (2, 4, 4, 4, 17, 2, 260, 33, 0, "bf16", "int8", True, True),
+    (1, 8, 4, 1, 30, 2, 520, 32, 1, "bf16", "e4m3", True, True),
+    (1, 2, 2, 2, 9, 1, 270, 250, 0, "bf16", "int8", False, True),
 ]
 
 
@@ -119,6 +129,25 @@ def test_attention(dev, B, H, Hkv, Hr, C, k, nQ, rows, lag, dtype, fmt, obo, hol
     g = _fill(c, C + k, lengths)
     idx, sel = _lists(rng, B, Hr, nQ, C, k, holes)
     q = torch.randn(B, H, nQ * rows, 64, generator=g, device=dev, dtype=_elem(dtype))
+    got = gca.cache_xattn(c, q, torch.from_numpy(idx).to(dev), torch.from_numpy(sel).to(dev), causal=bool(lag))
+    _check_xattn(c, q, idx, sel, got, rows, lag)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attention_random_problems(dev, seed):
+    """Small problems drawn over everything a call may vary in."""
+    import torch
+    from paper_2410_01651_amd import gca
+    rng = np.random.default_rng(1000 + seed)
+    pick = lambda *a: a[rng.integers(len(a))]  # noqa: E731
+    Hkv, G, B = pick(1, 2, 3), pick(1, 2, 4, 5), pick(1, 2, 3)
+    C, k, nQ, rows = pick(1, 4, 30, 90), int(rng.integers(1, 33)), pick(1, 1, 2, 7), pick(1, 2, 5, 16, 31, 64, 70)
+    dtype, fmt, obo, lag = pick("bf16", "fp32"), pick("e4m3", "int8"), bool(pick(0, 1)), pick(0, 1)
+    c = gca.cache(B, G * Hkv, C, k, Hkv=Hkv, Hr=pick(1, Hkv), D=64, dtype=dtype, format=fmt, off_by_one=obo,
+                  attn_scale=pick(None, 0.3, -0.05))
+    g = _fill(c, seed, rng.integers(-1, 66, (B, C)).astype(np.int32))
+    idx, sel = _lists(rng, B, c.struct.Hr, nQ, C, k, True)
+    q = torch.randn(B, G * Hkv, nQ * rows, 64, generator=g, device=dev, dtype=_elem(dtype))
     got = gca.cache_xattn(c, q, torch.from_numpy(idx).to(dev), torch.from_numpy(sel).to(dev), causal=bool(lag))
     _check_xattn(c, q, idx, sel, got, rows, lag)
 
