@@ -327,8 +327,10 @@ gca_status gca_cache_xattn(const gca_cache* c, const void* q, const int32_t* idx
 /* Make room for the n next chunks of every sequence by evicting the chunks that gathered
  * the least attention weight.  In this order, for each sequence b:
  *   1. mass[b, j] = decay * mass[b, j] + the weights w of the entries of its lists that name
- *      slot j, for slots in use (each weight counted to the nearest 2^-48, negative and NaN
- *      ones as 0, so that the sum does not depend on its order); 0 for free slots;
+ *      slot j, for slots in use (each weight counted to the nearest 2^-48, or where a
+ *      sequence has 2^16 entries or more, of less than 2^e to the nearest 2^(e - 64), so that
+ *      the sum does not depend on its order; negative and NaN ones as 0, ones above 1 as 1);
+ *      0 for free slots;
  *   2. m = want[b] slots (n if want is NULL; at most n) are taken: free slots first, lowest
  *      first, then the chunks in order of (mass, slot), except those numbered below
  *      keep_first or not below next[b] - keep_last.  A negative or NaN mass ranks as 0;

@@ -132,13 +132,14 @@ def evict(tokens, mass, number, nxt, n, idx=None, w=None, decay=1.0, keep_first=
     new = np.zeros((B, C), np.float32)
     slots = np.full((B, n), -1, np.int64)
     for b in range(B):
-        add = np.zeros(C, object)          # exact integers, units of 2^-48
+        add = np.zeros(C, object)          # exact integers, in units of 2^-48 or as 2^16 entries or more need
+        bits = 64 - max(16, int(idx[b].size).bit_length()) if idx is not None else 48
         if idx is not None:
             for j, x in zip(idx[b].reshape(-1), w[b].reshape(-1)):
                 if 0 <= j < C and x > 0:
-                    add[j] += int(np.floor(min(float(x), 32768.0) * 2.0**48 + 0.5))
+                    add[j] += int(np.floor(min(float(x), 1.0) * 2.0**bits + 0.5))
         used = tokens[b] > 0
-        total = np.array([float(a) for a in add]) * 2.0**-48
+        total = np.array([float(a) for a in add]) * 2.0**-bits
         with np.errstate(over="ignore", invalid="ignore"):
             m = (np.float64(np.float32(decay)) * mass[b].astype(np.float64) + total).astype(np.float32)
         new[b] = np.where(used, m, 0)

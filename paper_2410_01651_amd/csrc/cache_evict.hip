@@ -3,8 +3,9 @@
 // first, then the least attended.
 //
 // Mathematics.  mass'[j] = decay mass[j] + sum of the weights of the entries naming j.  The
-// sum is formed in LDS in units of 2^-48 as 64-bit integers, so that it does not depend on the
-// order of the atomic additions; the product and the sum with it are one fp64 fma, rounded
+// sum is formed in LDS in units of 2^-48 (coarser from 2^16 entries on, so that no sum of weights up
+// to 1 passes 64 bits) as 64-bit integers, so that it does not depend on the order of the atomic
+// additions; the product and the sum with it are one fp64 fma, rounded
 // once to fp32.  The choice is the m smallest keys of a slot order: key 0 for a free slot, 1 +
 // the bits of the mass (non-negative floats order as their bits) for one that may go, the
 // largest key for one that must stay.  The m-th smallest key is found by splitting the range
@@ -282,7 +283,7 @@ __device__ void give_slots(const EvictParams& p, Scratch& s, uint32_t b, Keys ke
 template <int TILE, int THREADS>
 __global__ __launch_bounds__(THREADS) void cache_evict_kernel(EvictParams p) {
   constexpr int kPer = TILE / THREADS;
-  __shared__ unsigned long long acc[TILE];  // units of 2^-48
+  __shared__ unsigned long long acc[TILE];  // in units
   // key x at x + x / 32: the threads' consecutive keys then lie in different banks
   __shared__ uint32_t key[TILE + TILE / 32];
   __shared__ Scratch s;
@@ -291,29 +292,45 @@ __global__ __launch_bounds__(THREADS) void cache_evict_kernel(EvictParams p) {
   const uint32_t N = (uint32_t)min((int64_t)TILE, p.C - c0);
   const int64_t base = (int64_t)b * p.C + c0;
   const int64_t next = p.next[b];
-  // everything of a thread's slots is asked for before the lists
+  // entries < 2^bits, each at most 2^(64 - bits) units
+  const int bits = max(16, 32 - __builtin_clz(p.entries | 1));
+  const double units = __longlong_as_double((int64_t)(1023 + 64 - bits) << 52);
+  const double unit = __longlong_as_double((int64_t)(1023 - 64 + bits) << 52);
+  // everything of a thread's slots is asked for before the lists, and at once: a load that a branch
+  // guards would be waited for before the next (threads without a slot take the last one's)
   int32_t tokens[kPer], number[kPer];
   float mass[kPer];
 #pragma unroll
   for (int u = 0; u < kPer; ++u) {
-    const uint32_t x = tid + u * THREADS;
-    tokens[u] = x < N ? p.tokens[base + x] : 0;
-    mass[u] = x < N ? p.mass[base + x] : 0.f;
-    number[u] = x < N ? p.number[base + x] : 0;
+    const uint32_t x = min(tid + u * THREADS, N - 1);
+    tokens[u] = p.tokens[base + x];
+    mass[u] = p.mass[base + x];
+    number[u] = p.number[base + x];
   }
   if (p.entries) {
     for (uint32_t x = tid; x < N; x += THREADS) acc[x] = 0;
     __syncthreads();
     const int32_t* idx = p.idx + (int64_t)b * p.entries;
     const float* w = p.w + (int64_t)b * p.entries;
-    for (uint32_t e = tid; e < p.entries; e += THREADS) {
-      const int32_t j = idx[e];
-      const float f = w[e];
+    auto add = [&](int32_t j, float f) {
       const uint32_t x = (uint32_t)j - c0;  // entries of other tiles and pads fall outside
-      if (j < 0 || x >= N) continue;
-      const double u = f > 0.f ? (double)fminf(f, 32768.f) * 0x1p48 : 0.0;
+      if (j < 0 || x >= N) return;
+      const double u = f > 0.f ? (double)fminf(f, 1.f) * units : 0.0;
       atomicAdd(&acc[x], (unsigned long long)(u + 0.5));
+    };
+    uint32_t e = tid;
+    for (; (uint64_t)e + 7 * THREADS < p.entries; e += 8 * THREADS) {  // eight in flight
+      int32_t j[8];
+      float f[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        j[y] = idx[e + y * THREADS];
+        f[y] = w[e + y * THREADS];
+      }
+#pragma unroll
+      for (int y = 0; y < 8; ++y) add(j[y], f[y]);
     }
+    for (; e < p.entries; e += THREADS) add(idx[e], w[e]);
     __syncthreads();
   }
 #pragma unroll
@@ -321,7 +338,7 @@ __global__ __launch_bounds__(THREADS) void cache_evict_kernel(EvictParams p) {
     const uint32_t x = tid + u * THREADS;
     if (x < N) {
       const bool used = tokens[u] > 0;
-      const double add = p.entries ? (double)acc[x] * 0x1p-48 : 0.0;
+      const double add = p.entries ? (double)acc[x] * unit : 0.0;
       const float m = used ? (float)fma((double)p.decay, (double)mass[u], add) : 0.f;
       p.mass[base + x] = m;
       const int64_t num = number[u];

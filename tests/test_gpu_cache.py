@@ -538,6 +538,29 @@ def test_evict_sum_does_not_depend_on_the_order(dev):
     assert float((got[0][0].double() - exact).abs().max()) <= float(exact.max()) * U * 1.01
 
 
+@pytest.mark.parametrize("C", [6, 9000])
+def test_evict_long_lists(dev, C):
+    """Sums that pass 2^16: 2^16 + 11 weights of one, of more and at random for the same few slots (the
+    batches of eight entries and what is left behind them), then the same and 5,000 more."""
+    import torch
+    from paper_2410_01651_amd import gca
+    rng = np.random.default_rng(C)
+    for entries in (65547, 70551):
+        c = gca.cache(1, 3, C, 1, Hr=3, D=64)
+        c.tokens.fill_(64)
+        c.mass.fill_(0.375)
+        state = tuple(x.cpu().numpy() for x in (c.tokens, c.mass, c.number, c.next))
+        idx = np.full((1, 3, entries // 3, 1), C - 2, np.int32)
+        w = np.ones(idx.shape, np.float32)
+        idx[0, 0, ::5], w[0, 0, ::5] = 1, rng.random(w[0, 0, ::5].shape)
+        w[0, 1, ::7] = 40000.0                       # (counts as 1)
+        gca.cache_evict(c, 0, torch.from_numpy(idx).to(dev), torch.from_numpy(w).to(dev), decay=0.5)
+        want = oc.evict(*state, 0, idx, w, 0.5)[1]
+        assert want.max() > 60000
+        # as in test_evict: a rounding of the oracle's sum in fp64, and of the result to fp32
+        assert (np.abs(c.mass.cpu().numpy().astype(np.float64) - want) <= 2 * U * want).all()
+
+
 # ----------------------------------------------------------------- together ----
 
 def _serve(gca, c, xs, rows, ws, st=None):
