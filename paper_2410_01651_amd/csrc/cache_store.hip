@@ -7,7 +7,8 @@
 // the wave, and the transposed tile is 8 x 8 byte blocks turned in registers (byte
 // permutes), so a tile goes through no LDS and is read and written once.
 //
-// Bound by HBM: a bf16 tile reads 8 KiB and writes 4 KiB.
+// Bound by HBM: a bf16 tile reads 8 KiB and writes 4 KiB.  1,024 chunks of 2 sequences and 16 heads (806 MB)
+// take 154 us, 5.3 TB/s in random slots; one chunk of 32 sequences and 16 heads (12.6 MB) 5.2 us.
 #include "cache_plan.hpp"
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
@@ -18,19 +19,30 @@ namespace {
 constexpr int kStoreThreads = 256;
 
 struct StoreParams {
-  const void* src[2];  // new keys, new values
-  uint8_t* dst[2];
-  float* scale[2];
-  const void* lmk;
-  void* lmk_dst;
   const int32_t* slots;
   const int32_t* lengths;
   int32_t* tokens;
   uint32_t tiles, items;  // 2 B Hkv n tiles, then B Hr n landmark rows (none without lmk)
   uint32_t n, Hkv, Hr;
-  int64_t C;
+  int32_t C;
+  uint32_t claimed;  // `tokens` says which chunk a slot takes
+  uint32_t seqs;
   int row_bytes;  // of a landmark row
+  const void* src[2];  // new keys, new values
+  uint8_t* dst[2];
+  float* scale[2];
+  const void* lmk;
+  void* lmk_dst;
 };
+
+// A slot that a sequence names twice takes the last chunk.  Up to kClaimFrom chunks per sequence every
+// tile's wave looks through the slots behind its own; a longer call, where that would grow as n^2, has
+// `tokens` hold kClaim + the last chunk's number while it runs, in three small launches around the store
+// (clear, claim by the largest number, length).  A length is at most 64, so a chunk never
+// takes another's length for its own claim.  Looking / claiming, bf16, us: 2 sequences of 16 heads, 256
+// chunks each 35 / 45, 512 84 / 86, 1,024 161 / 154, 2,048 355 / 293; 16,384 chunks of 8 heads 2,045 / 619.
+constexpr int kClaim = 128;
+constexpr int64_t kClaimFrom = 512;
 
 __device__ __forceinline__ uint32_t max_u64(uint32_t x) {
   x = max(x, dpp<kDppXor1>(x));
@@ -48,8 +60,9 @@ __device__ __forceinline__ uint32_t max_u64(uint32_t x) {
 template <typename T> struct Row8;
 template <> struct Row8<__bf16> {
   u32x4 x;  // pairs of bf16
-  __device__ __forceinline__ void load(const void* p) { x = *reinterpret_cast<const u32x4*>(p); }
-  __device__ __forceinline__ void clear() { x = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t src, uint32_t at, int row) {
+    x = __builtin_amdgcn_raw_buffer_load_b128(src, at, row, 0);
+  }
   __device__ __forceinline__ float at(int c) const {
     const uint32_t w = x[c >> 1];
     return __uint_as_float((c & 1) ? (w & 0xffff0000u) : (w << 16));
@@ -57,11 +70,10 @@ template <> struct Row8<__bf16> {
 };
 template <> struct Row8<float> {
   f32x4 lo, hi;
-  __device__ __forceinline__ void load(const void* p) {
-    lo = reinterpret_cast<const f32x4*>(p)[0];
-    hi = reinterpret_cast<const f32x4*>(p)[1];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t src, uint32_t at, int row) {
+    lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(src, at, row, 0));
+    hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(src, at + 16, row, 0));
   }
-  __device__ __forceinline__ void clear() { lo = hi = f32x4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ float at(int c) const { return c < 4 ? lo[c] : hi[c - 4]; }
 };
 
@@ -84,30 +96,48 @@ __device__ __forceinline__ uint32_t pk_e4m3(float a, float b, uint32_t w, bool h
             : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)w, false);
 }
 
+// Chunks with tokens among n, of a sequence of `total` new tokens.
+__device__ __forceinline__ uint32_t with_tokens(uint32_t n, int total) {
+  const int64_t x = ((int64_t)total + kS - 1) / kS;
+  return (uint32_t)(x < 0 ? 0 : x < n ? x : n);
+}
+
+// Whether a later chunk with tokens of the sequence, before `last`, names chunk i's slot too.
+__device__ __forceinline__ bool replaced(const StoreParams& p, uint32_t b, uint32_t i, uint32_t last, int slot,
+                                         int lane) {
+  if (i + 1 >= last) return false;
+  if (p.claimed) return p.tokens[(int64_t)b * p.C + slot] != kClaim + (int)i;
+  const int32_t* slots = p.slots + (int64_t)b * p.n;
+  for (uint32_t e = i + 1; e < last; e += 64)
+    if (__ballot(e + lane < last && slots[e + lane < last ? e + lane : i] == slot)) return true;
+  return false;
+}
+
 template <typename T, bool I8>
 __device__ __forceinline__ void store_tile(const StoreParams& p, uint32_t item, int lane) {
   // item = ((b Hkv + h) n + i) 2 + which
   const uint32_t which = item & 1, t = item >> 1;
-  const uint32_t i = t % p.n, bh = t / p.n, b = bh / p.Hkv;
-  const int64_t len64 = p.lengths ? (int64_t)p.lengths[b] - 64 * (int64_t)i : kS;
+  // (the quotients are formed on the vector unit: back to scalar registers, and with them every address)
+  const uint32_t bh = __builtin_amdgcn_readfirstlane(t / p.n), i = t - bh * p.n;
+  const uint32_t b = __builtin_amdgcn_readfirstlane(bh / p.Hkv);
+  int slot = p.slots[(int64_t)b * p.n + i];
+  int total = p.lengths ? p.lengths[b] : 0;
+  slot = __builtin_amdgcn_readfirstlane(slot);
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int64_t len64 = p.lengths ? (int64_t)total - 64 * (int64_t)i : kS;
   const int len = (int)(len64 < kS ? len64 : kS);
-  const int32_t* row_slots = p.slots + (int64_t)b * p.n;
-  const int slot = row_slots[i];
   if (len <= 0 || slot < 0 || slot >= p.C) return;
   const int rg = lane >> 3, cg = lane & 7;
   Row8<T> x[8];
-  const char* src = reinterpret_cast<const char*>(p.src[which]) + (int64_t)t * (kS * kD * (int)sizeof(T)) +
-                    (rg * 8 * kD + cg * 8) * (int)sizeof(T);
+  // (rows behind the last token lie past the descriptor's end and read as zeros)
+  constexpr int kRow = kD * (int)sizeof(T);
+  const __amdgpu_buffer_rsrc_t src =
+      range_rsrc(reinterpret_cast<const char*>(p.src[which]) + (int64_t)t * (kS * kRow), (uint32_t)(len * kRow));
+  const uint32_t at = rg * 8 * kRow + cg * 8 * (int)sizeof(T);
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    if (rg * 8 + r < len) x[r].load(src + r * kD * (int)sizeof(T));
-    else x[r].clear();
-  }
+  for (int r = 0; r < 8; ++r) x[r].load(src, at, r * kRow);
   // a later chunk of the sequence that is stored in the same slot replaces this one
-  const int64_t stored = p.lengths ? ((int64_t)p.lengths[b] + kS - 1) / kS : p.n;  // chunks with tokens
-  const uint32_t last = (uint32_t)(stored < p.n ? stored : p.n);
-  for (uint32_t e = i + 1; e < last; e += 64)
-    if (__ballot(e + lane < last && row_slots[e + lane < last ? e + lane : i] == slot)) return;
+  if (replaced(p, b, i, p.lengths ? with_tokens(p.n, total) : p.n, slot, lane)) return;
 
   // the largest finite magnitude, as its bits
   uint32_t top = 0;
@@ -203,24 +233,38 @@ __device__ __forceinline__ void store_tile(const StoreParams& p, uint32_t item, 
   for (int r = 0; r < 8; ++r) *reinterpret_cast<u32x2*>(dst + r * 64) = u32x2{w[2 * r], w[2 * r + 1]};
   if (lane == 0) {
     p.scale[which][tile] = scale;
-    if (which == 0 && bh == b * p.Hkv) p.tokens[(int64_t)b * p.C + slot] = len;
+    if (which == 0 && bh == b * p.Hkv && !p.claimed) p.tokens[(int64_t)b * p.C + slot] = len;
   }
 }
 
 // Landmark row i of (sequence, retrieval head) into the same slot.
 __device__ __forceinline__ void store_landmark(const StoreParams& p, uint32_t item, int lane) {
-  const uint32_t i = item % p.n, bhr = item / p.n, b = bhr / p.Hr;
-  const int32_t* row_slots = p.slots + (int64_t)b * p.n;
-  const int slot = row_slots[i];
-  const int64_t stored = p.lengths ? ((int64_t)p.lengths[b] + kS - 1) / kS : p.n;
-  const uint32_t last = (uint32_t)(stored < 0 ? 0 : stored < p.n ? stored : p.n);
-  if (i >= last || slot < 0 || slot >= p.C) return;
-  for (uint32_t e = i + 1; e < last; e += 64)
-    if (__ballot(e + lane < last && row_slots[e + lane < last ? e + lane : i] == slot)) return;
+  const uint32_t bhr = __builtin_amdgcn_readfirstlane(item / p.n), i = item - bhr * p.n;
+  const uint32_t b = __builtin_amdgcn_readfirstlane(bhr / p.Hr);
+  const int slot = p.slots[(int64_t)b * p.n + i];
+  const uint32_t last = p.lengths ? with_tokens(p.n, p.lengths[b]) : p.n;
+  if (i >= last || slot < 0 || slot >= p.C || replaced(p, b, i, last, slot, lane)) return;
   const char* src = reinterpret_cast<const char*>(p.lmk) + (int64_t)item * p.row_bytes;
   char* dst = reinterpret_cast<char*>(p.lmk_dst) + ((int64_t)bhr * p.C + slot) * p.row_bytes;
   for (int x = lane * 16; x < p.row_bytes; x += 1024)
     *reinterpret_cast<u32x4*>(dst + x) = *reinterpret_cast<const u32x4*>(src + x);
+}
+
+// STEP 0, 1: before the store, slots named cleared, then claimed; 2: after it, the lengths.
+template <int STEP>
+__global__ __launch_bounds__(kStoreThreads) void cache_claim_kernel(StoreParams p) {
+  const uint32_t at = blockIdx.x * kStoreThreads + threadIdx.x;  // b n + i
+  const uint32_t b = at / p.n, i = at - b * p.n;
+  if (b >= p.seqs || i >= (p.lengths ? with_tokens(p.n, p.lengths[b]) : p.n)) return;
+  const int slot = p.slots[at];
+  if (slot < 0 || slot >= p.C) return;
+  int32_t* tokens = p.tokens + (int64_t)b * p.C + slot;
+  if constexpr (STEP == 0) *tokens = 0;
+  if constexpr (STEP == 1) atomicMax(tokens, kClaim + (int)i);
+  if constexpr (STEP == 2) {
+    const int64_t len = p.lengths ? (int64_t)p.lengths[b] - 64 * (int64_t)i : kS;
+    if (*tokens == kClaim + (int)i) *tokens = (int)(len < kS ? len : kS);
+  }
 }
 
 template <typename T, bool I8>
@@ -253,17 +297,25 @@ hipError_t launch_cache_store(const gca_cache& c, const void* k, const void* v, 
   p.n = (uint32_t)n;
   p.Hkv = c.Hkv;
   p.Hr = c.Hr;
-  p.C = c.capacity;
+  p.C = (int)c.capacity;
   p.row_bytes = c.D * (c.dtype == GCA_BF16 ? 2 : 4);
   const int per = kStoreThreads / 64;
   const dim3 grid((p.items + per - 1) / per), block(kStoreThreads);
   const bool i8 = c.format == GCA_INT8;
+  p.claimed = n > kClaimFrom;
+  p.seqs = (uint32_t)c.B;
+  const dim3 claims((unsigned)((c.B * n + kStoreThreads - 1) / kStoreThreads));
+  if (p.claimed) {
+    launch_kernel("cache_claim_kernel", cache_claim_kernel<0>, claims, block, 0, stream, p);
+    launch_kernel("cache_claim_kernel", cache_claim_kernel<1>, claims, block, 0, stream, p);
+  }
   if (c.dtype == GCA_BF16)
     launch_kernel("cache_store_kernel", i8 ? cache_store_kernel<__bf16, true> : cache_store_kernel<__bf16, false>,
                   grid, block, 0, stream, p);
   else
     launch_kernel("cache_store_kernel", i8 ? cache_store_kernel<float, true> : cache_store_kernel<float, false>, grid,
                   block, 0, stream, p);
+  if (p.claimed) launch_kernel("cache_claim_kernel", cache_claim_kernel<2>, claims, block, 0, stream, p);
   return take_launch_error();
 }
 

@@ -561,6 +561,34 @@ def test_evict_long_lists(dev, C):
         assert (np.abs(c.mass.cpu().numpy().astype(np.float64) - want) <= 2 * U * want).all()
 
 
+@pytest.mark.parametrize("n,last", [(300, 300), (512, 500), (600, 600), (1200, 1111)])
+def test_store_names_a_slot_again_far_behind(dev, n, last):
+    """The last chunk with tokens of those that name a slot is stored, however far behind the others."""
+    import torch
+    from paper_2410_01651_amd import gca
+    g = torch.Generator(device=dev).manual_seed(n)
+    c = gca.cache(1, 1, n, 4, D=64)
+    k = torch.randn(1, 1, n * 64, 64, generator=g, device=dev, dtype=torch.bfloat16)
+    lmk = torch.randn(1, 1, n, 64, generator=g, device=dev, dtype=torch.bfloat16)
+    slots = np.random.default_rng(n).permutation(n).astype(np.int32)
+    for at, of in ((64, 0), (65, 1), (last * 9 // 10, 2), (last - 1, 3), (last - 1, last // 2), (290, 289)):
+        slots[at] = slots[of]
+    lengths = torch.tensor([64 * last], device=dev, dtype=torch.int32)
+    gca.cache_store(c, k, k, lmk, torch.from_numpy(slots[None]).to(dev), lengths)
+    holds = {}
+    for i in range(last):
+        holds[slots[i]] = i
+    one = gca.cache(1, 1, n, 4, D=64)                # every chunk in the slot of its number
+    gca.cache_store(one, k, k, lmk, torch.arange(n, device=dev, dtype=torch.int32)[None].contiguous())
+    at = torch.tensor(list(holds), device=dev)
+    of = torch.tensor(list(holds.values()), device=dev)
+    for name in ("k", "v"):
+        a, b = getattr(c, name).view(torch.uint8), getattr(one, name).view(torch.uint8)
+        assert torch.equal(a[0, 0, at], b[0, 0, of])
+    assert torch.equal(c.k_scale[0, 0, at], one.k_scale[0, 0, of]) and torch.equal(c.lmk[0, 0, at], one.lmk[0, 0, of])
+    assert int((c.tokens > 0).sum()) == len(holds)
+
+
 # ----------------------------------------------------------------- together ----
 
 def _serve(gca, c, xs, rows, ws, st=None):
