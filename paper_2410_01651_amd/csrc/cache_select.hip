@@ -89,25 +89,34 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(const float*
   __shared__ uint64_t result[kMergeWaves][32];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = blockIdx.x;
-  const float* rs = ls + row * lists * K;
+  const int* score_bits = reinterpret_cast<const int*>(ls) + row * lists * K;
   const int* rj = lj + row * lists * K;
   const int64_t share = (lists + kMergeWaves - 1) / kMergeWaves;
   const int64_t l_lo = wave * share, l_hi = l_lo + share < lists ? l_lo + share : lists;
-  auto entry = [&](int64_t at) -> uint64_t {
-    const float v = rs[at];
-    const int j = rj[at];
-    return j >= 0 ? pack_key(v, j) : 0;
+  // entry `at` of the row, 0 if not wanted.  The loads are made on every path and all before the
+  // first use (the empty asm): one that a branch guards is waited for before the next.
+  auto ask = [&](bool wanted, int64_t at, int& v, int& j) {
+    at = wanted ? at : 0;
+    v = score_bits[at];
+    j = rj[at];
+  };
+  auto got = [&](bool wanted, int v, int j) { return wanted && j >= 0 ? pack_key(__int_as_float(v), j) : 0; };
+  auto entry = [&](bool wanted, int64_t at) -> uint64_t {
+    int v, j;
+    ask(wanted, at, v, j);
+    asm volatile("" : "+v"(v), "+v"(j));
+    return got(wanted, v, j);
   };
   Best best(buf[wave], K);
   if (share * K <= 64) {
     // an entry per lane
     const int l = lane / K;
-    best.start(l_lo + l < l_hi && l < share ? entry(l_lo * K + lane) : 0);
+    best.start(entry(l_lo + l < l_hi && l < share, l_lo * K + lane));
   } else {
     if (share <= 64) {
-      best.start(l_lo + lane < l_hi ? entry((l_lo + lane) * K) : 0);
+      best.start(entry(l_lo + lane < l_hi, (l_lo + lane) * K));
     } else {
-      for (int64_t l0 = l_lo; l0 < l_hi; l0 += 64) best.offer(l0 + lane < l_hi ? entry((l0 + lane) * K) : 0);
+      for (int64_t l0 = l_lo; l0 < l_hi; l0 += 64) best.offer(entry(l0 + lane < l_hi, (l0 + lane) * K));
       best.settle();
     }
     // lane s < K: the list that the s-th best head heads
@@ -115,15 +124,21 @@ __global__ __launch_bounds__(kMergeThreads) void cache_merge_kernel(const float*
     const int list = head != 0 ? (int)scan_list_of(key_chunk(head), pw) : -1;
     if (K * K <= 64) {
       const int l = __shfl(list, lane / K);
-      best.start(lane < K * K && l >= 0 ? entry((int64_t)l * K + lane % K) : 0);
+      best.start(entry(lane < K * K && l >= 0, (int64_t)l * K + lane % K));
     } else {
       bool more = list >= 0;
       for (int r = 1; r < K; r += 4) {
+        int v[4], j[4];
         uint64_t x[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = more && r + u < K ? entry((int64_t)list * K + r + u) : 0;
+        for (int u = 0; u < 4; ++u) ask(more && r + u < K, (int64_t)list * K + r + u, v[u], j[u]);
+        asm volatile(""
+                     : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(j[0]), "+v"(j[1]), "+v"(j[2]), "+v"(j[3]));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) best.offer(x[u]);
+        for (int u = 0; u < 4; ++u) {
+          x[u] = got(more && r + u < K, v[u], j[u]);
+          best.offer(x[u]);
+        }
         more = more && x[3] > best.bar;  // (else nothing behind it can join)
         if (__ballot(more) == 0) break;
       }
