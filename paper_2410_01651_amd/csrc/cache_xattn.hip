@@ -31,29 +31,32 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr int kMaxWaves = 8;
 constexpr int kTileBytes = kS * kD;
 
+// (in the order of use)
 struct XattnParams {
-  const uint8_t* k;
-  const uint8_t* v;
-  const float* ks;
-  const float* vs;
-  const int32_t* tokens;
-  const void* q;
+  uint32_t items, blocks;  // work items; row blocks per group
+  uint32_t nw;             // waves per item
+  uint32_t nQ, Hkv, Hr;
+  int topk, lag, C;
+  uint32_t H, G, rows, M;  // M = G rows: query rows of a group that share a cached head
+  uint32_t part;           // bytes of LDS before the partial outputs
   const int32_t* idx;
   const float* sel;
+  const int32_t* tokens;
+  const float* ks;
+  const float* vs;
+  const uint8_t* k;
+  const uint8_t* v;
+  const void* q;
   void* out;
   float* lse;
   float* w;
-  uint32_t items, blocks;  // work items; row blocks per group
-  uint32_t nQ, H, Hkv, Hr, G, rows, M;  // M = G rows: query rows of a group that share a cached head
-  uint32_t part;  // bytes of LDS before the partial outputs
-  int topk, lag, off_by_one, C;
-  float scale;  // |attn_scale| log2 e
+  float scale;      // |attn_scale| log2 e
   uint32_t negate;  // the sign bits of one query entry (fp32) or two, if attn_scale < 0
+  int off_by_one;
 };
 
 __device__ __forceinline__ f32x16 mma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
@@ -122,6 +125,15 @@ __device__ __forceinline__ void store8(float* p, const float* x) {
   reinterpret_cast<f32x4*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
 }
 
+// A wave-uniform address in scalar registers.  (As a pointer to global memory: through an integer it would
+// lose that, and a wait for a load that might be from elsewhere is a wait for all loads.)
+template <typename T>
+__device__ __forceinline__ __attribute__((address_space(1))) T* scalar_ptr(T* x) {
+  return reinterpret_cast<__attribute__((address_space(1))) T*>(uniform_addr(x));
+}
+
+// (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
+// floating point flags and would be called.)
 // T: type of the queries; W: MFMA tile; NC: column blocks of W query rows.
 template <typename T, bool I8, int W, int NC>
 __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnParams p) {
@@ -138,10 +150,11 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   typedef __attribute__((ext_vector_type(NR))) float Acc;
   extern __shared__ __attribute__((aligned(16))) float smem[];
 
-  const uint32_t it = (uint32_t)xcd_swizzle(blockIdx.x, gridDim.x);
+  const uint32_t it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
   if (it >= p.items) return;
-  const int lane = threadIdx.x & 63, g = lane / W, col = lane % W;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
+  const uint32_t tid = __builtin_amdgcn_workitem_id_x(), nw = p.nw, threads = 64 * nw;
+  const int lane = tid & 63, g = lane / W, col = lane % W;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // item = ((b Hkv + h) nQ + t) blocks + block
   // (the quotients are formed on the vector unit: back to scalar registers, and with them every address)
   auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
@@ -174,22 +187,17 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   const bool has_list = (int)t >= p.lag;
   const uint32_t list = has_list ? t - p.lag : p.nQ - 1;
   const int64_t row = ((int64_t)b * p.Hr + (p.Hr == 1 ? 0 : h)) * p.nQ + list;
-  int j = -1;
-  float sv = -INFINITY;
-  if (lane < K) {
-    j = reinterpret_cast<const int32_t*>(uniform_addr(p.idx + row * K))[lane];
-    sv = reinterpret_cast<const float*>(uniform_addr(p.sel + row * K))[lane];
-  }
-  const bool named = j >= 0 && j < p.C;
+  // (loads on every path, lanes behind the list's end taking its last entry's: one that a branch
+  // guards is waited for before the next)
+  const uint32_t mine_at = min(lane, K - 1);
+  int j = scalar_ptr(p.idx + row * K)[mine_at];
+  const float sv = scalar_ptr(p.sel + row * K)[mine_at];
+  const bool named = lane < K && j >= 0 && j < p.C;
   j = named ? j : 0;
   const int64_t slot0 = (int64_t)bh * p.C;
-  int length = 0;
-  float kscale = 0.f, vscale = 0.f;
-  if (named) {
-    length = reinterpret_cast<const int32_t*>(uniform_addr(p.tokens + (int64_t)b * p.C))[(uint32_t)j];
-    kscale = reinterpret_cast<const float*>(uniform_addr(p.ks + slot0))[(uint32_t)j];
-    vscale = reinterpret_cast<const float*>(uniform_addr(p.vs + slot0))[(uint32_t)j];
-  }
+  int length = scalar_ptr(p.tokens + (int64_t)b * p.C)[(uint32_t)j];
+  float kscale = scalar_ptr(p.ks + slot0)[(uint32_t)j];
+  float vscale = scalar_ptr(p.vs + slot0)[(uint32_t)j];
 
   // The first tiles that the list names for this wave are asked for at once, beside their lengths
   // and scales: it is nearly always so that they are in use.
@@ -215,12 +223,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const uint32_t m = min(uint32_t(c * W + col), p.M - 1 - m0);
-    const T* qr = reinterpret_cast<const T*>(uniform_addr(reinterpret_cast<const T*>(p.q) + row0 * kD)) + ahead(m) * kD;
+    const auto* qr = scalar_ptr(reinterpret_cast<const T*>(p.q) + row0 * kD) + ahead(m) * kD;
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
-      const T* src = qr + 16 * (g + NG * (s >> 1)) + 8 * (s & 1);
+      const auto* src = qr + 16 * (g + NG * (s >> 1)) + 8 * (s & 1);
       if constexpr (kB16) {
-        u32x4 x = *reinterpret_cast<const u32x4*>(src);
+        u32x4 x = *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(src);
         x ^= u32x4{p.negate, p.negate, p.negate, p.negate};
         qf[c][s][0] = __builtin_bit_cast(bf16x8, x);
       } else {
@@ -240,7 +248,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   }
 
   // ---- fusion weights (Eq. 2)
-  length = max(min(length, kS), 0);
+  length = named ? max(min(length, kS), 0) : 0;
   const bool valid = length > 0;
   vscale = valid ? vscale : 0.f;  // (a free slot's scale may be anything)
   const float top = max64(valid ? sv : -INFINITY);
@@ -258,7 +266,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   const uint32_t nrows = min((uint32_t)QB, p.M - m0);
   float* const lse_s = smem;  // [row][entry]
   if (p.lse) {
-    for (uint32_t e = threadIdx.x; e < nrows * K; e += blockDim.x) lse_s[e] = -INFINITY;
+    for (uint32_t e = tid; e < nrows * K; e += threads) lse_s[e] = -INFINITY;
     __syncthreads();
   }
 
@@ -394,7 +402,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
 
   // ---- output: value u of a lane is column 32 (u / 16) + 16 g + u % 16 (W = 32) or 16 g + u
   const float osc = vmax > 0.f ? vmax * 0x1p-15f : 1.f;
-  T* const out0 = reinterpret_cast<T*>(uniform_addr(reinterpret_cast<T*>(p.out) + row0 * kD));
+  T* const out0 = (T*)scalar_ptr(reinterpret_cast<T*>(p.out) + row0 * kD);
   if (nw == 1) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -430,7 +438,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
       }
     }
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < nrows * 16; e += blockDim.x) {
+    for (uint32_t e = tid; e < nrows * 16; e += threads) {
       const uint32_t m = e >> 4, x = e & 15;
       f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
       for (uint32_t y = 0; y < waves; ++y)
@@ -439,8 +447,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
     }
   }
   if (p.lse) {
-    float* const dst = reinterpret_cast<float*>(uniform_addr(p.lse + row0 * K));
-    for (uint32_t e = threadIdx.x; e < nrows * K; e += blockDim.x) {
+    float* const dst = (float*)scalar_ptr(p.lse + row0 * K);
+    for (uint32_t e = tid; e < nrows * K; e += threads) {
       const uint32_t m = flat ? 0 : e / K;
       dst[flat ? (int64_t)e : ahead(m) * K + (e - m * K)] = lse_s[e];
     }
@@ -505,6 +513,7 @@ hipError_t launch_cache_xattn(const gca_cache& c, const void* q, const int32_t* 
   while (nw < kMaxWaves && 2 * nw <= c.topk && (int64_t)p.items * nw < 8 * device_cus() &&
          p.part + 2 * nw * rb * kD * sizeof(float) <= 65536)
     nw *= 2;
+  p.nw = (uint32_t)nw;
   const size_t lds = p.part + (nw > 1 ? (size_t)nw * rb * kD * sizeof(float) : 0);
   const dim3 grid((p.items + 7) / 8 * 8), block(64 * nw);
   auto run = [&](auto tag, auto i8) {
