@@ -589,6 +589,44 @@ def test_store_names_a_slot_again_far_behind(dev, n, last):
     assert int((c.tokens > 0).sum()) == len(holds)
 
 
+@pytest.mark.parametrize("fmt,dt", [("e4m3", "bf16"), ("int8", "fp32")])
+def test_store_long_is_store_in_pieces(dev, fmt, dt):
+    """One call of 700 chunks (captured and replayed with other slots, too) leaves what two calls of 350
+    leave: slots named twice and outside the cache, sequences that end early, late or have nothing."""
+    import torch
+    from paper_2410_01651_amd import gca
+    rng = np.random.default_rng(7)
+    B, H, Hr, n, C = 4, 2, 2, 700, 900
+    g = torch.Generator(device=dev).manual_seed(8)
+    one, two = (gca.cache(B, H, C, 4, Hr=Hr, D=64, format=fmt, dtype=dt) for _ in range(2))
+    for c in (one, two):
+        c.tokens.fill_(3)
+    k, v = (torch.randn(B, H, n * 64, 64, generator=g, device=dev).to(one.elem) for _ in range(2))
+    lmk = torch.randn(B, Hr, n, 64, generator=g, device=dev).to(one.elem)
+    half = lambda x, i: x.view(B, x.shape[1], 2, -1, 64)[:, :, i].contiguous()  # noqa: E731
+    pieces = [(half(k, i), half(v, i), half(lmk, i)) for i in range(2)]
+    slots = torch.zeros(B, n, dtype=torch.int32, device=dev)
+    lengths = torch.tensor([0, 64 * 400 + 5, 64 * n, 64 * n + 999], dtype=torch.int32, device=dev)
+    st = torch.cuda.Stream()
+    gr = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(gr, stream=st):
+        gca.cache_store(one, k, v, lmk, slots, lengths=lengths)
+    for turn in range(4):
+        slots.copy_(torch.from_numpy(rng.integers(-5, C + 5, (B, n)).astype(np.int32)))
+        torch.cuda.synchronize()
+        if turn == 0:
+            gca.cache_store(one, k, v, lmk, slots, lengths=lengths)
+        else:
+            gr.replay()
+        for i, piece in enumerate(pieces):
+            gca.cache_store(two, *piece, slots[:, 350 * i:350 * (i + 1)].contiguous(),
+                            lengths=(lengths - 64 * 350 * i).clamp(0, 64 * 350 + (999 if i else 0)))
+        torch.cuda.synchronize()
+        for x in one.NAMES:
+            assert torch.equal(getattr(one, x).view(torch.uint8), getattr(two, x).view(torch.uint8)), (turn, x)
+
+
 # ----------------------------------------------------------------- together ----
 
 def _serve(gca, c, xs, rows, ws, st=None):
