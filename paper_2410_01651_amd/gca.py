@@ -436,6 +436,7 @@ class Cache:
         self.ref = ctypes.byref(struct)
         self.device = device
         self.index = index    # the device's ordinal
+        self.here = _Here(torch, index)
         self.dims = struct.B, struct.H, struct.Hkv, struct.Hr, struct.D, struct.topk
         self.elem = torch.bfloat16 if struct.dtype == GCA_BF16 else torch.float32
         for name in self.NAMES:
@@ -495,31 +496,48 @@ def cache_workspace(c: Cache, op: int, n: int = 0):
     return _torch().empty(max(size, 1), dtype=_torch().uint8, device=c.device), size
 
 
-class _At:
-    """Context in which a cache's call allocates and launches, with the stream's handle as its
-    value: the given stream, or the current one of the cache's device, which is made the current
-    device if it is not."""
+class _Here:
+    """Context of a cache's call on the current stream of its device, which is the current one; the
+    value is the stream's handle.  (One per cache: it holds nothing of a call.)"""
 
-    def __init__(self, c: Cache, stream):
-        torch = c.torch
-        self.ctx = None
-        if stream is None:
-            if torch.cuda.current_device() != c.index:
-                self.ctx = torch.cuda.device(c.index)
-            self.raw = torch._C._cuda_getCurrentRawStream(c.index)
-        else:
-            if stream.device != c.device:
-                raise ValueError(f"the stream is on {stream.device}, the cache on {c.device}")
-            self.ctx, self.raw = torch.cuda.stream(stream), stream.cuda_stream
+    __slots__ = ("raw", "index")
+
+    def __init__(self, torch, index):
+        self.raw, self.index = torch._C._cuda_getCurrentRawStream, index
 
     def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        return self.raw
+        return self.raw(self.index)
 
     def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+        pass
+
+
+class _There:
+    """The same on another stream or another device's: made current while the call allocates and
+    launches."""
+
+    def __init__(self, ctx, c: Cache):
+        self.ctx, self.c = ctx, c
+
+    def __enter__(self):
+        self.ctx.__enter__()
+        return self.c.here.__enter__()
+
+    def __exit__(self, *exc):
+        self.ctx.__exit__(*exc)
+
+
+def _at(c: Cache, stream):
+    """Context in which a cache's call allocates and launches: on the given stream, or the current
+    one of the cache's device."""
+    torch = c.torch
+    if stream is None:
+        if torch._C._cuda_getDevice() == c.index:
+            return c.here
+        return _There(torch.cuda.device(c.index), c)
+    if stream.device != c.device:
+        raise ValueError(f"the stream is on {stream.device}, the cache on {c.device}")
+    return _There(torch.cuda.stream(stream), c)
 
 
 def _cache_ptr(c: Cache, t, name, dtype, shape):
@@ -553,7 +571,7 @@ def cache_store(c: Cache, k, v, lmk, slots, lengths=None, stream=None):
         raise ValueError("slots must have shape (B, n)")
     n = slots.shape[1]
     kv = (B, Hkv, n * 64, 64)
-    with _At(c, stream) as st:
+    with _at(c, stream) as st:
         _check(lib().gca_cache_store(c.ref, _cache_ptr(c, k, "k", c.elem, kv), _cache_ptr(c, v, "v", c.elem, kv),
                                      _cache_ptr(c, lmk, "lmk", c.elem, (B, Hr, n, D)),
                                      _cache_ptr(c, slots, "slots", i32, (B, n)),
@@ -568,7 +586,7 @@ def cache_select(c: Cache, lmk_q, idx=None, sel=None, w=None, want_w=True, ws=No
     rows = (B, Hr, 1, K)
     qp, ip = _cache_ptr(c, lmk_q, "lmk_q", c.elem, (B, Hr, 1, D)), _cache_ptr(c, idx, "idx", i32, rows)
     sp, wp = _cache_ptr(c, sel, "sel", f32, rows), _cache_ptr(c, w, "w", f32, rows)
-    with _At(c, stream) as st:
+    with _at(c, stream) as st:
         if idx is None:
             idx, ip = _new(c, rows, i32)
         if sel is None:
@@ -597,7 +615,7 @@ def cache_xattn(c: Cache, q, idx, sel, out=None, lse=None, w=None, want_lse=True
     qp, ip = _cache_ptr(c, q, "q", c.elem, qs), _cache_ptr(c, idx, "idx", i32, rows)
     sp, op = _cache_ptr(c, sel, "sel", f32, rows), _cache_ptr(c, out, "out", c.elem, qs)
     lp, wp = _cache_ptr(c, lse, "lse", f32, ls), _cache_ptr(c, w, "w", f32, rows)
-    with _At(c, stream) as st:
+    with _at(c, stream) as st:
         if out is None:
             out, op = _new(c, qs, c.elem, q)
         if lse is None and want_lse:
@@ -622,7 +640,7 @@ def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_las
     rows = (B, Hr, nQ, K)
     ip, wp = _cache_ptr(c, idx, "idx", i32, rows), _cache_ptr(c, w, "w", f32, rows)
     want_p, sp = _cache_ptr(c, want, "want", i32, (B,)), _cache_ptr(c, slots, "slots", i32, (B, n))
-    with _At(c, stream) as st:
+    with _at(c, stream) as st:
         if slots is None:
             slots, sp = _new(c, (B, n), i32)
         if ws is None:
