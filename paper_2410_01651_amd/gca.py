@@ -557,8 +557,9 @@ def _cache_ptr(c: Cache, t, name, dtype, shape):
 
 
 def _new(c: Cache, shape, dtype, like=None):
-    """A new output and its address (nothing to check); `like`: a tensor of its shape and type."""
-    t = c.torch.empty(shape, dtype=dtype, device=c.device) if like is None else c.torch.empty_like(like)
+    """A new output and its address (nothing to check); `like`: a tensor of its shape, which is cheaper
+    to go by."""
+    t = c.torch.empty(shape, dtype=dtype, device=c.device) if like is None else c.torch.empty_like(like, dtype=dtype)
     return t, t.data_ptr()
 
 
@@ -588,9 +589,9 @@ def cache_select(c: Cache, lmk_q, idx=None, sel=None, w=None, want_w=True, ws=No
     sp, wp = _cache_ptr(c, sel, "sel", f32, rows), _cache_ptr(c, w, "w", f32, rows)
     with _at(c, stream) as st:
         if idx is None:
-            idx, ip = _new(c, rows, i32)
+            idx, ip = _new(c, rows, i32, sel)
         if sel is None:
-            sel, sp = _new(c, rows, f32)
+            sel, sp = _new(c, rows, f32, idx)
         if w is None and want_w:
             w, wp = _new(c, rows, f32, sel)
         if ws is None:
