@@ -424,6 +424,39 @@ def test_select(dev, B, Hkv, Hr, C, k, D, dtype, share):
     assert (np.abs(host64(w) - rw) <= (4 * err + 64 * U) * rw).all()
 
 
+@pytest.mark.parametrize("C,k,D,dtype", [(1, 1, 64, "bf16"), (7, 8, 192, "fp32"), (8, 32, 320, "bf16"), (9, 3, 1024, "bf16"),
+                                         (64, 8, 576, "bf16"), (65, 32, 256, "fp32"), (129, 8, 2048, "bf16"),
+                                         (255, 16, 64, "fp32"), (256, 32, 1024, "bf16"), (256, 8, 768, "fp32"),
+                                         (257, 8, 128, "bf16"), (250, 8, 2048, "bf16"), (20, 8, 8192, "fp32")])
+def test_select_small_caches(dev, C, k, D, dtype):
+    """Both sides of the borders of the form for small caches (256 slots, 768 KiB of landmarks per row)."""
+    test_select(dev, 3, 2, 2, C, k, D, dtype, 0.8)
+
+
+@pytest.mark.parametrize("C", [30, 200])
+def test_select_small_caches_ties(dev, C):
+    """Ties go to the lower slot; scores that are not finite are no candidates; an empty cache has none."""
+    import torch
+    from paper_2410_01651_amd import gca
+    g = torch.Generator(device=dev).manual_seed(C)
+    D, k = 192, 6
+    c = gca.cache(2, 1, C, k, D=D)
+    c.lmk.copy_(torch.randn(c.lmk.shape, generator=g, device=dev) * 0.1)
+    lq = torch.randn(2, 1, 1, D, generator=g, device=dev, dtype=torch.bfloat16)
+    same = [3, 4, 11, 12, 17, C - 3, C - 2]
+    for j in same:
+        c.lmk[:, 0, j] = lq[:, 0, 0]                                   # the best of all, seven times
+    c.lmk[0, 0, 5, 0], c.lmk[0, 0, 6, 191], c.lmk[0, 0, 7] = float("nan"), float("inf"), float("-inf")
+    c.tokens.fill_(64)
+    idx, sel, w = gca.cache_select(c, lq)
+    assert idx[:, 0, 0].tolist() == [same[:6]] * 2 and torch.equal(sel, sel[..., :1].expand_as(sel))
+    assert float((w - 1 / 6).abs().max()) <= 4 * U / 6                 # exp(0) = 1, a sum of six, one division
+    c.tokens[0, 4], c.tokens[1] = 0, -1
+    idx, sel, w = gca.cache_select(c, lq)
+    assert idx[0, 0, 0].tolist() == [3, 11, 12, 17, C - 3, C - 2]
+    assert (idx[1] == -1).all() and (sel[1] == float("-inf")).all() and (w[1] == 0).all()
+
+
 def test_select_equals_the_decode_path(dev):
     """A full cache retrieves what gca_forward in DECODE mode does; ties go to the lower slot, and
     landmarks whose scores are not finite are not candidates."""
