@@ -317,9 +317,10 @@ gca_status gca_cache_select(const gca_cache* c, const void* lmk_q, int32_t* idx,
  *   lse [B, H, nQ * rows, topk] fp32   output: log of each entry's softmax denominator
  *                                      (-inf on pads), may be NULL
  *   w   [B, Hr, nQ, topk]       fp32   output: fusion weights of every list, may be NULL
- * Products of q with the cached numbers are exact and summed in fp32; probabilities are
- * rounded to fp16 (fp32 tensors: to two fp16 terms), and in any case to no less than 2^-40,
- * before they meet the values.
+ * Products of q with the cached numbers are exact and summed in fp32.  Probabilities, with
+ * their entry's fusion weight and value scale in them, are rounded to fp16 (fp32 tensors: to
+ * two fp16 terms), but not finer than to a 2^-40th of the list's largest product of weight
+ * and value scale, before they meet the values.
  * Requires c->k, v, k_scale, v_scale, tokens. */
 gca_status gca_cache_xattn(const gca_cache* c, const void* q, const int32_t* idx, const float* sel, void* out,
                            float* lse, float* w, int64_t nQ, int64_t rows, int32_t lag, hipStream_t stream);

@@ -84,14 +84,15 @@ def weights(idx, sel, tokens):
 
 
 def xattn(q, idx, sel, k, v, k_scale, v_scale, tokens, attn_scale, rows, lag=0, off_by_one=False):
-    """Dict out, lse, w, and three bounds' ingredients: `mag` = sum_s w sum_keys p |v| and `num` =
-    (largest value scale of the list) x sum_s sum_keys |number| (both of out's shape), and `dot` =
-    the largest sum |attn_scale q k| over the row's valid entries [B, H, Lq]."""
+    """Dict out, lse, w, and four bounds' ingredients: `mag` = sum_s w sum_keys p |v|, `num` =
+    (largest value scale of the list) x sum_s sum_keys |number| and `wnum`, the same with the largest
+    product of value scale and fusion weight (all of out's shape), and `dot` = the largest
+    sum |attn_scale q k| over the row's valid entries [B, H, Lq]."""
     B, H, Lq, d = q.shape
     Hkv = k.shape[1]
     _, Hr, nQ, K = idx.shape
     ok, w = weights(idx, sel, tokens)
-    out, mag, num = np.zeros((B, H, Lq, d)), np.zeros((B, H, Lq, d)), np.zeros((B, H, Lq, d))
+    out, mag, num, wnum = (np.zeros((B, H, Lq, d)) for _ in range(4))
     lse = np.full((B, H, Lq, K), NEG_INF)
     dot = np.zeros((B, H, Lq))
     for b in range(B):
@@ -103,6 +104,8 @@ def xattn(q, idx, sel, k, v, k_scale, v_scale, tokens, attn_scale, rows, lag=0, 
                 qq = q[b, h, r].astype(np.float64)
                 top = max((float(v_scale[b, kv, j]) for j, o in zip(idx[b, hr, t - lag], ok[b, hr, t - lag]) if o),
                           default=0.0)
+                wtop = max((float(v_scale[b, kv, j]) * x for j, o, x in
+                            zip(idx[b, hr, t - lag], ok[b, hr, t - lag], w[b, hr, t - lag]) if o), default=0.0)
                 for s in range(K):
                     if not ok[b, hr, t - lag, s]:
                         continue
@@ -121,8 +124,9 @@ def xattn(q, idx, sel, k, v, k_scale, v_scale, tokens, attn_scale, rows, lag=0, 
                     out[b, h, r] += w[b, hr, t - lag, s] * (p @ vv)
                     mag[b, h, r] += w[b, hr, t - lag, s] * (p @ np.abs(vv))
                     num[b, h, r] += top * np.abs(v[b, kv, j, :, :n]).sum(axis=1)
+                    wnum[b, h, r] += wtop * np.abs(v[b, kv, j, :, :n]).sum(axis=1)
                     lse[b, h, r, s] = (m + np.log(den))[:, 0]
-    return dict(out=out, lse=lse, w=w, mag=mag, num=num, dot=dot)
+    return dict(out=out, lse=lse, w=w, mag=mag, num=num, wnum=wnum, dot=dot)
 
 
 def evict(tokens, mass, number, nxt, n, idx=None, w=None, decay=1.0, keep_first=0, keep_last=0, want=None):

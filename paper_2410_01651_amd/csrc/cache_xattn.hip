@@ -3,10 +3,10 @@
 //
 // Mathematics.  For slot j of a list, K_j = kappa_j N_j and V_j = nu_j M_j with 8-bit numbers
 // N, M, so  s = (attn_scale kappa_j) q N_j^T,  P = softmax(s) over the chunk's tokens, and
-// out = sum_j w_j P V_j = nu sum_j (w_j nu_j / nu) P M_j  with nu the largest of the list's
-// nu_j.  Every e4m3 number and every int8 is exact in bf16 and in fp16, so the scales stay out
+// out = sum_j w_j P V_j = u sum_j (w_j nu_j / u) P M_j  with u a power of two, by the list's largest
+// w_j nu_j.  Every e4m3 number and every int8 is exact in bf16 and in fp16, so the scales stay out
 // of the operands: q N^T is a product of exact operands with fp32 sums (fp32 queries: three
-// bf16 terms, 24 bits), and the scaled probabilities (w_j nu_j / nu) P 2^15 <= 2^15 meet M in
+// bf16 terms, 24 bits), and the scaled probabilities (w_j nu_j / u) P < 65,473 meet M in
 // fp16, 11 bits each (fp32 tensors: two fp16 terms, 22 bits).  As every chunk has a softmax of its own,
 // nothing is rescaled and the slots of a list can be split over waves and added.
 //
@@ -261,8 +261,14 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   const float total = sum64(es);
   const float wl = valid ? es / total : 0.f;
   if (p.w && wave == 0 && blk == 0 && (p.Hr != 1 || h == 0) && lane < K) p.w[row * K + lane] = wl;
-  const float vmax = max64(vscale);
-  const float coef = vmax > 0.f ? wl * (vscale / vmax) * 0x1p15f : wl * vscale;
+  // c_j = w_j nu_j as mantissa and exponent, since the product may lie outside fp32's range.  All are scaled
+  // by the power of two 2^(16 - top_octave) that brings the largest into [1023 / 2048, 1023 / 1024) 2^16,
+  // which fp16 holds.  (By the products: a chunk that hardly counts may have any value scale.)
+  const float mant = __builtin_amdgcn_frexp_mantf(wl) * __builtin_amdgcn_frexp_mantf(vscale);
+  const int expo = __builtin_amdgcn_frexp_expf(wl) + __builtin_amdgcn_frexp_expf(vscale);
+  const int octave = expo + __builtin_amdgcn_frexp_expf(mant * (1024.f / 1023.f));
+  const int top_octave = __builtin_amdgcn_readfirstlane((int)max64(mant != 0.f ? (float)octave : -1000.f));
+  const float coef = __builtin_ldexpf(mant, expo - top_octave + 16);
   const uint64_t all = __ballot(valid && has_list);
   const uint32_t count = __popcll(all);
   uint32_t mine = share(all);
@@ -406,7 +412,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
   }
 
   // ---- output: value u of a lane is column 32 (u / 16) + 16 g + u % 16 (W = 32) or 16 g + u
-  const float osc = vmax > 0.f ? vmax * 0x1p-15f : 1.f;
+  const auto unscale = [&](float x) { return __builtin_ldexpf(x, top_octave - 16); };
   T* const out0 = (T*)scalar_ptr(reinterpret_cast<T*>(p.out) + row0 * kD);
   if (nw == 1) {
 #pragma unroll
@@ -418,7 +424,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
       for (int u = 0; u < NV; u += 8) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = o[c][(u + e) / NR][(u + e) % NR] * osc;
+        for (int e = 0; e < 8; ++e) x[e] = unscale(o[c][(u + e) / NR][(u + e) % NR]);
         store8(dst + (u / 16) * 32 + u % 16, x);
       }
     }
@@ -448,7 +454,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void cache_xattn_kernel(XattnPar
       f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
       for (uint32_t y = 0; y < waves; ++y)
         acc += *reinterpret_cast<const f32x4*>(part + (y * nrows + m) * kD + 4 * (x ^ (m & 15)));
-      store4(out0 + ahead(m) * kD + 4 * x, acc[0] * osc, acc[1] * osc, acc[2] * osc, acc[3] * osc);
+      store4(out0 + ahead(m) * kD + 4 * x, unscale(acc[0]), unscale(acc[1]), unscale(acc[2]), unscale(acc[3]));
     }
   }
   if (p.lse) {
