@@ -309,7 +309,9 @@ gca_status gca_cache_select(const gca_cache* c, const void* lmk_q, int32_t* idx,
  * group t attends to the chunks of list t - lag: lag = 0 gives every group the list of its
  * own number, lag = 1 the one before (CAUSAL lists; group 0 then has none).  Entries that
  * name no slot in use (outside [0, capacity), or tokens <= 0) are pads; a slot's softmax
- * is over its first `tokens` keys.  Rows without a valid entry get out = 0.
+ * is over its first `tokens` keys.  Rows without a valid entry get out = 0.  NaN in a query
+ * row, or in the keys, values or scales of an entry's tokens, comes out as NaN; what lies
+ * behind a slot's tokens or in free slots has no effect, whatever it is.
  *   q   [B, H, nQ * rows, d]    dtype
  *   idx [B, Hr, nQ, topk]       int32
  *   sel [B, Hr, nQ, topk]       fp32   finite on valid entries

@@ -78,3 +78,91 @@ def test_scales_at_the_ends_of_their_range(dev, dtype, rows, power):
     assert torch.equal(torch.where(want.abs() >= 2.0**-126, out.double(), want), want)
     assert torch.equal(lse, one[1]) and torch.equal(w, one[2])
     _check_output(c, q, idx, sel, out, rows)
+
+
+# ---------------------------------------------------------------------- NaN ----
+
+def _fits(groups):
+    """Groups of 64 rows of one head for each form: 16, 32 and (from about 2,048 groups on) 64 rows per item."""
+    return dict(token=(1, 1), rows=(1, 40), prompt=(groups, 64))
+
+
+@pytest.mark.parametrize("fmt,dtype,form", [("e4m3", "bf16", "token"), ("e4m3", "bf16", "rows"), ("e4m3", "bf16", "prompt"),
+                                            ("e4m3", "fp32", "token"), ("e4m3", "fp32", "rows"), ("int8", "bf16", "token"),
+                                            ("int8", "bf16", "rows"), ("int8", "bf16", "prompt"), ("int8", "fp32", "token"),
+                                            ("int8", "fp32", "rows")])
+@pytest.mark.parametrize("obo", [False, True])
+def test_nan_in_use_comes_through(dev, fmt, dtype, form, obo):
+    """NaN keys, values and scales of chunks that a list names, and NaN query rows, reach what depends
+    on them by the formula and nothing else: every row of a list with a NaN key (or key scale), the value's
+    column of it (or all, for a value scale), a query's own row."""
+    import torch
+    from paper_2410_01651_amd import gca
+    nQ, rows = _fits(2100)[form]
+    C, k = 6, 3
+    c = gca.cache(1, 1, C, k, D=64, dtype=dtype, format=fmt, off_by_one=obo)
+    g = _fill(c, 3, np.array([[64, 40, 64, 64, 64, 64]], np.int32))
+    # list t: slots 0, 1 and 2 or 3; slot 3 gets the NaN
+    idx = torch.tensor([0, 1, 2], dtype=torch.int32, device=dev).repeat(nQ, 1)
+    idx[1::2, 2] = 3
+    if nQ == 1:
+        idx[0, 2] = 3
+    idx = idx.view(1, 1, nQ, k).contiguous()
+    named = (idx == 3).any(dim=-1).view(nQ)
+    sel = torch.tensor([0.25, 1.0, -0.5], device=dev).repeat(nQ, 1).view(1, 1, nQ, k).contiguous()
+    q = torch.randn(1, 1, nQ * rows, 64, generator=g, device=dev, dtype=_elem(dtype))
+    want = gca.cache_xattn(c, q, idx, sel)
+    nan = float("nan")
+
+    def check(out_nan, lse_nan):
+        out, lse, w = gca.cache_xattn(c, q, idx, sel)
+        assert torch.equal(torch.isnan(out).view(nQ, rows, 64), out_nan.expand(nQ, rows, 64))
+        assert torch.equal(torch.isnan(lse).view(nQ, rows, k), lse_nan.expand(nQ, rows, k))
+        assert torch.equal(w, want[2])
+        for x, y in ((out, want[0]), (lse, want[1])):
+            assert torch.equal(torch.where(torch.isnan(x), y, x), y)
+
+    none = torch.zeros(1, 1, 1, dtype=torch.bool, device=dev)
+    row = named.view(nQ, 1, 1)
+    third = torch.arange(k, device=dev) == 2
+    column = torch.arange(64, device=dev) == 37
+    if fmt == "e4m3":
+        for t, at, o, s in ((c.k, (0, 0, 3, 50, 7), row, row & third), (c.v, (0, 0, 3, 37, 50), row & column, none)):
+            was = t.view(torch.uint8)[at].clone()
+            t.view(torch.uint8)[at] = 0xFF
+            check(o, s)
+            t.view(torch.uint8)[at] = was
+    for t, s in ((c.k_scale, row & third), (c.v_scale, none)):
+        was = t[0, 0, 3].clone()
+        t[0, 0, 3] = nan
+        check(row, s)
+        t[0, 0, 3] = was
+    q[0, 0, -1, 9] = nan
+    mine = torch.zeros(nQ, rows, 1, dtype=torch.bool, device=dev)
+    mine[-1, -1] = True
+    check(mine, mine)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_nan_stored_is_nan_attended(dev, fmt, dtype):
+    """A NaN among a stored chunk's tokens comes back from the attention; one behind its length does not."""
+    import torch
+    from paper_2410_01651_amd import gca
+    g = torch.Generator(device=dev).manual_seed(2)
+    slots = torch.zeros(1, 1, dtype=torch.int32, device=dev)
+    q = torch.randn(1, 1, 3, 64, generator=g, device=dev, dtype=_elem(dtype))
+    sel = torch.zeros(1, 1, 1, 1, device=dev)
+    for which in (0, 1):
+        kv = [torch.randn(1, 1, 64, 64, generator=g, device=dev, dtype=_elem(dtype)) for _ in range(2)]
+        kv[which][0, 0, 20, 11] = float("nan")
+        for length in (21, 20):
+            c = gca.cache(1, 1, 2, 1, D=64, dtype=dtype, format=fmt)
+            gca.cache_store(c, *kv, None, slots, lengths=torch.tensor([length], dtype=torch.int32, device=dev))
+            bad = torch.isnan(gca.cache_xattn(c, q, slots.view(1, 1, 1, 1), sel)[0])
+            if length == 20:
+                assert not bad.any()
+            elif which == 0 or fmt == "int8":
+                assert bad.all()
+            else:
+                assert bad[..., 11].all() and int(bad.sum()) == 3
