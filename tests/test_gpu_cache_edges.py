@@ -166,3 +166,58 @@ def test_nan_stored_is_nan_attended(dev, fmt, dtype):
                 assert bad.all()
             else:
                 assert bad[..., 11].all() and int(bad.sum()) == 3
+
+
+# ------------------------------------------------------------------- select ----
+
+SELECT = [
+    # B, Hr, C, k, what a lane of the scan does: it keeps each of its up to n scores (n <= k), or a running
+    # list of its best (up to 8, 16 or 32).  From 129 rows on a workgroup scans a row, so a lane sees C / 256.
+    (129, 1, 500, 8),      # 2
+    (65, 2, 1000, 5),      # 4
+    (129, 1, 1900, 8),     # 8
+    (129, 1, 3900, 20),    # 16
+    (65, 2, 7000, 32),     # 28
+    (129, 1, 1500, 2),     # list of 8
+    (256, 1, 4096, 8),
+    (65, 2, 3000, 9),      # list of 16
+    (129, 1, 4700, 16),
+    (129, 1, 5000, 17),    # list of 32
+    (65, 2, 9000, 32),
+    (2, 1, 262144, 5),     # a list of 8, 512 lists to merge
+    (1, 1, 262144, 3),
+    (3, 1, 200000, 2),
+]
+
+
+@pytest.mark.parametrize("B,Hr,C,k", SELECT)
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (512, "bf16"), (128, "fp32")])
+def test_select_every_form_of_the_scan(dev, B, Hr, C, k, D, dtype):
+    """Landmarks of small integers and a scale that is a power of two: every score is exact, so the
+    selection and its many ties are equal to the last bit; free slots everywhere, a free end, an
+    empty cache."""
+    import torch
+    from paper_2410_01651_amd import gca
+    g = torch.Generator(device=dev).manual_seed(C + k)
+    integers = lambda *s: torch.randint(-4, 5, s, generator=g, device=dev).to(_elem(dtype))  # noqa: E731
+    c = gca.cache(B, Hr, C, k, Hr=Hr, D=D, dtype=dtype, score_scale=2.0**-4)
+    for b in range(B):
+        c.lmk[b] = integers(Hr, C, D)
+    lq = integers(B, Hr, 1, D)
+    c.tokens.copy_(torch.randint(-2, 5, c.tokens.shape, generator=g, device=dev))
+    c.tokens[0, C // 2:] = 0
+    if B > 1:
+        c.tokens[1] = 0
+    c.lmk[0, :, C // 2:] = float("nan")     # (free: whatever is there)
+    idx, sel, w = gca.cache_select(c, lq)
+    for b in range(B):
+        s = (c.lmk[b].double() * lq[b].double()).sum(dim=-1) * 2.0**-4          # [Hr, C]
+        s = torch.where(c.tokens[b] > 0, s, float("-inf"))
+        m = min(k, int((c.tokens[b] > 0).sum()))
+        j = torch.sort(s, dim=1, descending=True, stable=True).indices[:, :m].sort(dim=1).values
+        top = torch.gather(s, 1, j)
+        assert torch.equal(idx[b, :, 0, :m].long(), j) and torch.equal(sel[b, :, 0, :m].double(), top), b
+        assert (idx[b, :, 0, m:] == -1).all() and (sel[b, :, 0, m:] == float("-inf")).all() and not w[b, :, 0, m:].any()
+        if m:      # exact exponents, 4 u each; the sum's and the quotient's roundings
+            p = torch.softmax(top, dim=1)
+            assert ((w[b, :, 0, :m].double() - p).abs() <= 64 * U * p + 2.0**-126).all()
