@@ -221,3 +221,18 @@ def test_select_every_form_of_the_scan(dev, B, Hr, C, k, D, dtype):
         if m:      # exact exponents, 4 u each; the sum's and the quotient's roundings
             p = torch.softmax(top, dim=1)
             assert ((w[b, :, 0, :m].double() - p).abs() <= 64 * U * p + 2.0**-126).all()
+
+
+# ------------------------------------------------------------------- evict ----
+
+@pytest.mark.parametrize("C,n", [
+    (30000, 136),     # 15 tiles' 2,040 candidates: 256 threads choose
+    (30000, 137),     # 2,055: 1,024 threads
+    (30000, 300),
+    (32768, 512),     # 8,192: the most that threads hold in registers
+    (32768, 513),     # 8,208: read again in every pass
+])
+@pytest.mark.parametrize("kind", ["ties", "wide", "plain"])
+def test_evict_every_form_of_the_merge(dev, C, n, kind):
+    from test_gpu_cache import test_evict
+    test_evict(dev, 2, 1, C, 8, 60, n, 0.75, 3, 5, kind)
