@@ -334,12 +334,15 @@ gca_status gca_cache_xattn(const gca_cache* c, const void* q, const int32_t* idx
  *      sequence has 2^16 entries or more, of less than 2^e to the nearest 2^(e - 64), so that
  *      the sum does not depend on its order; negative and NaN ones as 0, ones above 1 as 1);
  *      0 for free slots;
- *   2. m = want[b] slots (n if want is NULL; at most n) are taken: free slots first, lowest
- *      first, then the chunks in order of (mass, slot), except those numbered below
- *      keep_first or not below next[b] - keep_last.  A negative or NaN mass ranks as 0;
- *   3. the slots taken are written to slots[b, 0 ..], ascending, padded with -1 where there
- *      are fewer than n; tokens and mass of each become 0 and number[b, slots[b, i]] =
- *      next[b] + i; then next[b] += m.
+ *   2. m = want[b] slots (n if want is NULL; between 0 and n) are asked for: free slots first,
+ *      lowest first, then the chunks in order of (mass, slot), except those numbered below
+ *      keep_first or not below next[b] - keep_last, so that fewer than m may be taken.  A
+ *      negative or NaN mass ranks as 0;
+ *   3. the slots taken are written to slots[b, 0 ..], ascending, padded with -1 up to n; tokens
+ *      and mass of each become 0 and number[b, slots[b, i]] = next[b] + i; then next[b] += m
+ *      (chunks that found no slot keep their numbers).
+ * m is to be the number of chunks that the sequence will store: a slot that nothing is stored
+ * in was emptied for nothing, and a number that no chunk has counts towards keep_last.
  * gca_cache_store then fills them.  With n = 0 only the masses change.
  *   idx, w [B, Hr, nQ, topk] int32, fp32  lists and fusion weights since the last call; both
  *                                         NULL (and nQ ignored): none

@@ -630,7 +630,8 @@ def cache_xattn(c: Cache, q, idx, sel, out=None, lse=None, w=None, want_lse=True
 def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_last=1, want=None, slots=None, ws=None,
                 stream=None):
     """gca_cache_evict: adds the weights w of the lists idx [B, Hr, nQ, topk] to the masses and
-    returns slots [B, n] for each sequence's next n chunks (want [B]: fewer for some)."""
+    returns slots [B, n] for each sequence's next n chunks (want [B]: the number of chunks that each
+    will store, where some have fewer)."""
     i32, f32 = c.torch.int32, c.torch.float32
     B, _, _, Hr, _, K = c.dims
     nQ = 0

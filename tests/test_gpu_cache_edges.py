@@ -236,3 +236,46 @@ def test_select_every_form_of_the_scan(dev, B, Hr, C, k, D, dtype):
 def test_evict_every_form_of_the_merge(dev, C, n, kind):
     from test_gpu_cache import test_evict
     test_evict(dev, 2, 1, C, 8, 60, n, 0.75, 3, 5, kind)
+
+
+@pytest.mark.parametrize("C", [12, 9000])
+def test_prompts_of_different_lengths(dev, C):
+    """Sequences that store different numbers of chunks ask for that many: nothing is evicted for chunks
+    that do not come, their numbers follow on one another, and the last ones are protected.  Where too few may
+    go, the chunks that found no slot keep their numbers."""
+    import torch
+    from paper_2410_01651_amd import gca
+    g = torch.Generator(device=dev).manual_seed(C)
+    B, n = 4, 6
+    c = gca.cache(B, 2, C, 4, D=64)
+    r = lambda *s: torch.randn(*s, generator=g, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    seen = np.zeros(B, np.int64)
+    for turn in range(6):
+        lengths = np.array([0, 1 + 37 * turn, 64 * n, 130])
+        chunks = -(-lengths // 64)
+        lt = torch.from_numpy(lengths.astype(np.int32)).to(dev)
+        was = {x: getattr(c, x).cpu().numpy().copy() for x in ("tokens", "mass", "number", "next")}
+        slots = gca.cache_evict(c, n, keep_last=2, want=(lt + 63) // 64)
+        t, m, num, nxt, rs = oc.evict(*was.values(), n, keep_last=2, want=chunks)
+        np.testing.assert_array_equal(slots.cpu().numpy(), rs)
+        gca.cache_store(c, r(B, 2, n * 64, 64), r(B, 2, n * 64, 64), r(B, 1, n, 64), slots, lengths=lt)
+        c.mass.copy_(torch.where(c.tokens > 0, torch.rand(c.mass.shape, generator=g, device=dev), 0.0))
+        seen += chunks
+        np.testing.assert_array_equal(c.next.cpu().numpy(), seen)
+        np.testing.assert_array_equal(c.number.cpu().numpy(), num)
+        tokens = c.tokens.cpu().numpy()
+        for b in range(B):
+            took = rs[b, :chunks[b]]
+            assert (took >= 0).all() and len(set(took)) == chunks[b] and (rs[b, chunks[b]:] == -1).all()
+            want = t[b].copy()
+            want[took] = np.minimum(64, lengths[b] - 64 * np.arange(chunks[b]))
+            np.testing.assert_array_equal(tokens[b], want)
+            held = np.sort(num[b][tokens[b] > 0])
+            assert len(held) == min(seen[b], C) and (held[-2:] == np.arange(seen[b])[-2:]).all()
+    # more chunks than may go: the cache's last four stay, so C - 4 slots are given
+    slots = gca.cache_evict(c, C, keep_last=4)
+    full = c.tokens.cpu().numpy()[2]
+    assert int((slots[2] >= 0).sum()) == C - min(4, C) and int((full > 0).sum()) == 4
+    given = slots[2][slots[2] >= 0].long()
+    np.testing.assert_array_equal(c.number[2, given].cpu().numpy(), seen[2] + np.arange(C - 4))
+    assert int(c.next[2]) == seen[2] + C
