@@ -1015,6 +1015,10 @@ __device__ __forceinline__ int64_t scan_list_of(int64_t c, int64_t pw) {
 // share (k better maxima would all beat it), so the wave merges the k-lists of
 // those lists, and wave 0 merges the waves' results.  Result in wave 0 as
 // wave_merge leaves it.  Scratch: sS/sJ/sCnt as merge_wave_results.
+// Up to 64 entries per wave are sorted as they are, up to 64 lists have their maxima found by
+// one sort.  The decode attention without / with these two forms, us: one row of 300 chunks, k = 8
+// 11.2 / 9.0, of 1,000 11.2 / 9.9; 8 rows of 1,000 11.4 / 10.3; 32 rows of 1,000, k = 8 21.9 / 18.7,
+// k = 16 34.8 / 27.0; 8 rows, k = 16 32.0 / 31.0, k = 32 79.2 / 77.9; 262,144 chunks (neither) 11.6 / 11.7.
 template <int KM, int NW>
 __device__ void merge_lists(const float* __restrict__ ls, const int* __restrict__ lj, int64_t row, int64_t lists,
                             int64_t pw, int K, float* sS, int* sJ, int* sCnt, float& ms, int& mj, int& cnt) {
