@@ -9,9 +9,14 @@ namespace gca {
 
 constexpr int64_t kMaxCapacity = 262144;
 
-// Eviction: one workgroup per sequence for up to kEvictWhole slots; a cache of more is cut into
-// tiles, and a second launch chooses among every tile's candidates.
+// Eviction: one workgroup per sequence for up to kEvictWhole slots (106 KB of LDS; 16,384 would not fit);
+// a cache of more is cut into tiles, and a second launch chooses among every tile's candidates.
+// Whole / in tiles, us: one sequence of 4,096 slots, one to go 6.5 / 9.1, of 8,192 7.7 / 10.3, 1,024 to go
+// 13.5 / 20.8; 64 of 8,192, 8 to go 12.9 / 14.7; 256 of 4,096 8.9 / 11.7, of 8,192 11.9 / 14.1.
 constexpr int kEvictWhole = 8192;
+// Of 1,024 / 2,048 / 4,096 slots, both launches: 16,384 slots, one to go 9.7 / 10.5 / 12.4; 4 sequences of
+// 50,000, 40 to go 16.7 / 16.4 / 20.4, 1,024 to go 155 / 74 / 42; 262,144 slots, 64 to go 43 / 21.4 / 21.7.
+// Caches of up to a tile take the smaller workgroup: 64 of 2,048 slots, 8 to go 10.8 / 9.9 / 11.3.
 constexpr int kEvictTile = 2048;
 inline int64_t evict_tiles(const gca_cache& c) {
   return c.capacity <= kEvictWhole ? 1 : (c.capacity + kEvictTile - 1) / kEvictTile;
