@@ -356,8 +356,10 @@ gca_status gca_cache_evict(const gca_cache* c, const int32_t* idx, const float* 
 
 #define GCA_OP_CACHE_SELECT 2
 #define GCA_OP_CACHE_EVICT 3
-/* Bytes of workspace `op` (GCA_OP_CACHE_SELECT, or GCA_OP_CACHE_EVICT of n chunks) needs;
- * 0 if c is invalid or needs none.  It depends on c's sizes alone and never falls as n grows. */
+/* Bytes of workspace that `op` (GCA_OP_CACHE_SELECT, or GCA_OP_CACHE_EVICT of n chunks) asks
+ * for; 0 if c is invalid or none is asked for.  It depends on c's sizes alone and never falls as
+ * n grows.  A selection asks for what the scan in two launches needs, also where the cache
+ * is small enough for the form in one launch, which leaves it unused. */
 size_t gca_cache_workspace_size(const gca_cache* c, int op, int64_t n);
 
 /* Profiling aid (outside the method).  While armed, the i-th kernel that libgca

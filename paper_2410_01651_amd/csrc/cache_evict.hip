@@ -17,8 +17,9 @@
 // keys in LDS.  A larger cache is cut into tiles of kEvictTile slots (more workgroups, so that a
 // few long caches spread over the chip); each leaves its n smallest in the workspace and a second
 // launch, one workgroup per sequence, chooses among them.  Bound by its chain of
-// dependent steps (a few barriers each): there are 16 bytes per slot to read.  32 sequences of
-// 256 slots, one to go: 4.1 us; 4 of 50,000, 40 to go: 9.3 + 5.7; 64 of 8,192, 8 to go: 13.8.
+// dependent steps (a few barriers each): there are 12 bytes per slot to read and 4 to write.
+// 32 sequences of 256 slots, one to go: 4.1 us; 64 of 8,192, 8 to go: 12.9; 4 of 50,000, 40 to go:
+// 9.2 + 5.7, 1,024 to go (more candidates than the registers hold, read again in every pass): 10.6 + 63.
 #include "cache_plan.hpp"
 #include "gca_device.hpp"
 #include "gca_launch.hpp"

@@ -2,8 +2,9 @@
 // landmark keys with the free slots left out (decode_scan.hpp, MASK), then one workgroup per
 // retrieval row merges the scan's lists into the row's best k and writes them ascending by
 // slot with their fusion weights.  The scan is bound by reading the landmarks once, the merge
-// by its chain of dependent steps.  Small caches take one launch (cache_select_few_kernel).  262,144 slots of width 512 bf16 43.6 us (6.1 TB/s) + 6.2, 32
-// sequences of 1,000 slots of width 1,024 14.7 + 3.9.
+// by its chain of dependent steps.  Small caches take one launch (cache_select_few_kernel).
+// 262,144 slots of width 512 bf16 43.6 us (6.1 TB/s) + 6.2, 32 sequences of 1,000 slots of width
+// 1,024 14.7 + 3.9, one sequence of 128 slots 5.8.
 //
 // The merge's waves each take a share of the lists and keep their best 64 candidates as one
 // sorted 64-bit key per lane.  Candidates that beat the k-th are gathered in LDS until there are

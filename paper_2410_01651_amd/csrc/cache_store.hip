@@ -8,7 +8,7 @@
 // permutes), so a tile goes through no LDS and is read and written once.
 //
 // Bound by HBM: a bf16 tile reads 8 KiB and writes 4 KiB.  1,024 chunks of 2 sequences and 16 heads (806 MB)
-// take 154 us, 5.3 TB/s in random slots; one chunk of 32 sequences and 16 heads (12.6 MB) 5.2 us.
+// take 154 us, 5.3 TB/s in random slots; one chunk of 32 sequences and 16 heads (12.6 MB) 4.4 us.
 #include "cache_plan.hpp"
 #include "gca_device.hpp"
 #include "gca_launch.hpp"

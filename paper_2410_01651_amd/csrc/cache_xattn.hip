@@ -9,6 +9,10 @@
 // bf16 terms, 24 bits), and the scaled probabilities (w_j nu_j / u) P < 65,473 meet M in
 // fp16, 11 bits each (fp32 tensors: two fp16 terms, 22 bits).  As every chunk has a softmax of its own,
 // nothing is rescaled and the slots of a list can be split over waves and added.
+// One fp16 term for bf16 tensors is a choice: with it a tenth of the outputs is the neighbour of the
+// bf16 that fp32 sums round to (1.67e-3 of fp64 in all, against 1.66e-3); two terms leave 2 in 10,000, but
+// take, one / two, us: a token 4.5 / 4.8, 64 rows of 32 sequences 11.8 / 14.1, a 64K
+// prompt 470 / 605 (a cold run).  fp32 tensors: 2.0e-7 of fp64 (fp32 sums alone: 1.5e-7).
 //
 // Layout.  The products are formed transposed, S^T = N Q^T and O^T = M^T P^T, on MFMA tiles of
 // W x W (W = 32, or 16 for at most 16 rows): lane l = W g + c has query row c as its column.
@@ -23,10 +27,11 @@
 // Work.  One workgroup per (sequence, cached head, group, block of rows); its waves take the
 // list's valid slots in turn.
 //
-// Bounds, 8 entries per list, bf16.  One token of 64 sequences and 16 heads: HBM, 67 MB of tiles in 13.6
-// us (4.9 TB/s); of one sequence: a chain of three trips to memory, 4.5 us.  A 64K prompt of 2
-// sequences and 16 heads: instruction issue, 398 us, 0.58 of the rate of a large matrix product (532 vector
-// instructions of which 32 are matrix ones per slot and 64 rows).
+// Bounds, 8 entries per list, bf16.  One token of 64 sequences and 16 heads: HBM, 67 MB of tiles in 13.4
+// us (5.0 TB/s); of one sequence: a chain of three trips to memory, 4.5 us.  A 64K prompt of 2
+// sequences and 16 heads: instruction issue, 400-415 us, 0.57 of the rate of a large matrix product (532
+// vector instructions of which 32 are matrix ones per slot and 64 rows); int8 452 us (more instructions to
+// unpack), fp32 800, int8 867 (2.5 times the products).
 #include "cache_plan.hpp"
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
@@ -519,7 +524,9 @@ hipError_t launch_cache_xattn(const gca_cache& c, const void* q, const int32_t* 
   const int rb = (int)(M < qb ? M : qb);
   p.part = lse ? (uint32_t)((rb * c.topk * sizeof(float) + 15) & ~size_t(15)) : 0u;
   // Waves per item: enough to fill the chip's eight waves per CU, no more than the list has
-  // entries, and at most 64 KiB of LDS.
+  // entries, and at most 64 KiB of LDS.  At most 4 / 8 / 16 (16-row items), one token, us: one sequence of 8
+  // heads, 8 entries 4.4 / 4.5 / 4.6, 16 5.6 / 5.4 / 6.2, 32 7.9 / 7.2 / 8.0; 16 sequences of 8 cached
+  // heads, int8, 16 entries 6.5 / 6.5 / 7.1.
   int nw = 1;
   while (nw < kMaxWaves && 2 * nw <= c.topk && (int64_t)p.items * nw < 8 * device_cus() &&
          p.part + 2 * nw * rb * kD * sizeof(float) <= 65536)
