@@ -279,3 +279,93 @@ def test_prompts_of_different_lengths(dev, C):
     given = slots[2][slots[2] >= 0].long()
     np.testing.assert_array_equal(c.number[2, given].cpu().numpy(), seen[2] + np.arange(C - 4))
     assert int(c.next[2]) == seen[2] + C
+
+
+# ----------------------------------------------------------------- together ----
+
+def _steps(gca, c, xs, n, st=None):
+    """A token's attention, then the end of up to n chunks, as a serving loop makes them."""
+    idx, sel, w = gca.cache_select(c, xs["lmk_q"], stream=st)
+    out, lse, _ = gca.cache_xattn(c, xs["q"], idx, sel, want_w=False, stream=st)
+    slots = gca.cache_evict(c, n, idx, w, decay=0.5, keep_last=2, want=xs["want"], stream=st)
+    gca.cache_store(c, xs["k"], xs["v"], xs["lmk"], slots, lengths=xs["lengths"], stream=st)
+    return idx, sel, w, out, lse, slots
+
+
+def _inputs(torch, g, dev, B, H, Hkv, D, n):
+    r = lambda *s: torch.randn(*s, generator=g, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    lengths = torch.randint(0, 64 * n + 1, (B,), generator=g, device=dev, dtype=torch.int32)
+    return dict(lmk_q=r(B, 1, 1, D), q=r(B, H, 1, 64), k=r(B, Hkv, n * 64, 64), v=r(B, Hkv, n * 64, 64), lmk=r(B, 1, n, D),
+                lengths=lengths, want=(lengths + 63) // 64)
+
+
+def _same(torch, a, b):
+    return all(torch.equal(getattr(a, x).view(torch.uint8), getattr(b, x).view(torch.uint8)) for x in a.NAMES)
+
+
+@pytest.mark.parametrize("C", [20, 256, 400])
+def test_small_caches_in_a_graph(dev, C):
+    """A captured step over caches that take the one-launch forms (and one that does not), which allocates its
+    own workspaces, replayed with other inputs and eager steps between: the state and outputs of eager
+    steps alone."""
+    import torch
+    from paper_2410_01651_amd import gca
+    B, H, Hkv, k, D, n = 3, 4, 2, 8, 512, 2
+    g = torch.Generator(device=dev).manual_seed(C)
+    c, e = (gca.cache(B, H, C, k, Hkv=Hkv, D=D) for _ in range(2))
+    xs = _inputs(torch, g, dev, B, H, Hkv, D, n)
+    gr = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(gr, stream=torch.cuda.Stream()):
+        res = _steps(gca, c, xs, n)
+    for turn in range(2 * C // n if C == 20 else 8):
+        new = _inputs(torch, g, dev, B, H, Hkv, D, n)
+        for x in xs:
+            xs[x].copy_(new[x])
+        torch.cuda.synchronize()
+        gr.replay()
+        want = _steps(gca, e, xs, n)
+        torch.cuda.synchronize()
+        for a, b in zip(res, want):
+            assert torch.equal(a, b), turn
+        assert _same(torch, c, e), turn
+
+
+def test_threads_side_by_side(dev):
+    """Two host threads, each with its cache and stream, at once: what they leave alone."""
+    import threading
+    import torch
+    from paper_2410_01651_amd import gca
+    B, H, Hkv, k, D, n, turns = 2, 4, 2, 5, 128, 3, 30
+    sizes = (60, 900)
+    inputs = []
+    for seed in range(2):
+        g = torch.Generator(device=dev).manual_seed(seed)
+        inputs.append([_inputs(torch, g, dev, B, H, Hkv, D, n) for _ in range(turns)])
+
+    def loop(c, st, xss, outs):
+        for xs in xss:
+            outs.append(_steps(gca, c, xs, n, st))
+        st.synchronize()
+
+    runs = []
+    for at_once in (False, True):
+        caches = [gca.cache(B, H, C, k, Hkv=Hkv, D=D) for C in sizes]
+        outs = [[], []]
+        torch.cuda.synchronize()
+        threads = [threading.Thread(target=loop, args=(c, torch.cuda.Stream(), xss, o))
+                   for c, xss, o in zip(caches, inputs, outs)]
+        for t in threads:
+            t.start()
+            if not at_once:
+                t.join()
+        for t in threads:
+            t.join()
+        torch.cuda.synchronize()
+        assert all(len(o) == turns for o in outs)
+        runs.append((caches, outs))
+    for a, b in zip(*(r[0] for r in runs)):
+        assert _same(torch, a, b)
+    for a, b in zip(*(r[1] for r in runs)):
+        for x, y in zip(a, b):
+            assert all(torch.equal(s, t) for s, t in zip(x, y))
