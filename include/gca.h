@@ -362,6 +362,125 @@ gca_status gca_cache_evict(const gca_cache* c, const int32_t* idx, const float* 
  * is small enough for the form in one launch, which leaves it unused. */
 size_t gca_cache_workspace_size(const gca_cache* c, int op, int64_t n);
 
+/* --------------------------------------------------------------- token window ----
+ *
+ * The tokens that a layer's self-attention looks back at (the sliding window, with linear biases, of
+ * Methodology / Model Architecture, beside the retrieved chunks), in 8 bits, for serving: every
+ * sequence has `capacity` rows.  The calls below append new tokens (one, a tree of drafted ones, or
+ * a prompt), attend with their queries, verify drafts against the target's probabilities, and
+ * keep the accepted ones.  As with the chunk cache all state is the caller's device memory, every
+ * count is read on the device, and calls on one window are ordered by the caller.
+ *
+ * length[b] counts the tokens of sequence b, the newest included; position p is in row
+ * p mod capacity (window > 0: a ring), or in row p if p < capacity (window = 0: all tokens are
+ * seen; those past the capacity are counted but neither kept nor seen).
+ *
+ * Numbers.  As in the chunk cache, but with one scale per token and cached head for its 64
+ * keys, and one for its 64 values: the least power of two (at least 2^-126) that brings the largest
+ * finite magnitude to at most 448 (GCA_E4M3), or that magnitude (at least 2^-100) over 127
+ * (GCA_INT8).  Infinities are stored as the largest number; a token with a NaN among its keys
+ * (values) has the scale NaN for its keys (values).
+ *
+ * B sequences; H query heads share Hkv cached heads, as in gca_cache.  Supported: d == 64, H a
+ * multiple of Hkv, capacity a multiple of 64 up to 2^24, window 0 .. capacity. */
+typedef struct {
+  int32_t B, H, Hkv;
+  int32_t d;
+  int64_t capacity;     /* rows per sequence */
+  int32_t window;       /* tokens that a row sees, itself included; 0: all */
+  float attn_scale;     /* multiplies <q, k> */
+  int32_t off_by_one;   /* 1: the softmax's denominator is 1 + its sum, as in gca_problem */
+  int32_t dtype;        /* gca_dtype of q, k, v, out */
+  int32_t format;       /* gca_format of the kept numbers */
+  uint32_t flags;       /* 0 */
+  void* k;              /* [B, Hkv, capacity, d] 8-bit keys */
+  void* v;              /* [B, Hkv, capacity / 64, d, 64] 8-bit values, transposed per 64 rows */
+  float* k_scale;       /* [B, Hkv, capacity]; GCA_E4M3: powers of two */
+  float* v_scale;       /* [B, Hkv, capacity] */
+  int32_t* length;      /* [B] tokens of each sequence so far */
+  int32_t* ticket;      /* [B, 2 H] zeros before the first call; every call leaves them so */
+} gca_window;
+
+/* Append T new tokens to every sequence: token i of sequence b becomes position length[b] + i, and
+ * length[b] grows by their number.  Where that exceeds a ring's capacity, the last `capacity` of
+ * them are kept.  No row of another position is written.
+ *   k, v    [B, Hkv, T, d] dtype
+ *   lengths [B]            int32  new tokens of each sequence, 0 .. T of which count; NULL: T
+ * Requires w->k, v, k_scale, v_scale, length, ticket. */
+gca_status gca_window_append(const gca_window* w, const void* k, const void* v, const int32_t* lengths, int64_t T,
+                             hipStream_t stream);
+
+/* Attention of the newest tokens (those of the last append), n_b = lengths[b] (NULL: T) of them, over the
+ * window.  With base = length[b] - n_b, row i is at position base + depth(i), its depth being i in a
+ * chain (parents NULL) and in a tree of drafted tokens its number of ancestors; it sees
+ *   - the positions p < base with p > base + depth(i) - window,
+ *   - itself and its ancestors (a chain: the new tokens before it) less than `window` levels above,
+ * with scores  attn_scale <q, k> + slopes[h] (position of the key - position of the row),
+ * one softmax over all of them, and out = softmax V.  Rows from n_b on, and rows that see nothing, get out = 0
+ * and lse = -inf.  What a row does not see has no effect on it, whatever it is (a value's number that is NaN,
+ * which gca_window_append never stores, in a row that others see aside).
+ *   q       [B, H, T, d] dtype
+ *   parents [B, T]       int32  of each node; entries outside 0 .. i - 1 make node i a root.  Needs
+ *                               T <= 64.  NULL: a chain, of any T
+ *   lengths [B]          int32  as for the append; may be NULL
+ *   slopes  [H]          fp32   may be NULL: 0
+ *   out     [B, H, T, d] dtype  output
+ *   lse     [B, H, T]    fp32   output: log of each row's softmax denominator; may be NULL
+ * In a ring, a row's window has to outlast the new tokens: window + T - 1 <= capacity (a
+ * longer prompt comes in pieces; GCA_ERR_INVALID).  Products of q with the kept numbers are exact and summed
+ * in fp32.  Probabilities relative to the row's largest so far, with their value scale in them, are rounded to
+ * fp16 (fp32 tensors: to two fp16 terms), but not finer than to a 2^-40th of the largest
+ * value scale that the row's block of rows has met.
+ * Requires w->k, v, k_scale, v_scale, length, ticket.  Workspace: gca_window_workspace_size(w, T)
+ * bytes, 256-byte aligned. */
+gca_status gca_window_attn(const gca_window* w, const void* q, const int32_t* parents, const int32_t* lengths,
+                           const float* slopes, void* out, float* lse, int64_t T, void* workspace, size_t ws_bytes,
+                           hipStream_t stream);
+
+/* Of the newest n_b = lengths[b] (NULL: T) tokens keep those that path names, in its order, and drop the
+ * others: token path[b, i] moves to position base + i, base = length[b] - n_b, and length[b] becomes
+ * base + m.  The path's m entries end at the first that is not larger than the one before, or is
+ * outside 0 .. n_b - 1 (-1 padding).
+ *   path    [B, n] int32, 0 <= n <= 64 (e.g. from gca_verify)
+ *   lengths [B]    int32, as for the append; may be NULL
+ * Requires w->k, v, k_scale, v_scale, length.  T >= 1; in a ring T <= capacity. */
+gca_status gca_window_keep(const gca_window* w, const int32_t* path, int64_t n, const int32_t* lengths, int64_t T,
+                           hipStream_t stream);
+
+/* Bytes of workspace that gca_window_attn of up to T tokens asks for; 0 if w is invalid or none is
+ * asked for.  It depends on w's sizes alone and never falls as T grows. */
+size_t gca_window_workspace_size(const gca_window* w, int64_t T);
+
+/* Verification of drafted tokens by rejection sampling, so that what is kept is distributed as the target's
+ * own samples.  Node 0 of sequence b's tree is its newest token, nodes 1 .. n_b - 1 are drafts; p[b, i] are
+ * the target's probabilities of the token behind node i, and q[b, i] those that node i's children
+ * were drawn from, independently (q NULL: the children were chosen, not drawn).  From node a = 0, with
+ * r = p[a] and z = 1, the children of a are tested in ascending order: child c, of token x, has
+ *   s = z q[a, x] (NULL: z)   and is accepted if u[c] s < r[x]:  then a = c, r = p[a], z = 1, and its
+ * children follow; otherwise
+ *   r = max(r - z q[a], 0), z = sum r   (NULL: z = max(z - r[x], 0), r[x] = 0).
+ * When no child is left, the next token is drawn from r: the first x whose partial sum r[0] + .. + r[x]
+ * exceeds u[0] sum r.  If r is zero everywhere, from p[a]; if that is too, next = -1.  Probabilities count
+ * as 0 where they are negative or NaN and as 1 above 1.  Products and differences are in fp64, and sums are of
+ * r to the nearest 2^-44, exactly: they do not depend on their order.
+ *   p, q    [B, T, V] fp32 (q may be NULL)
+ *   tokens  [B, T]    int32  drafted tokens; one outside 0 .. V - 1 is rejected, leaving r as it is
+ *   parents [B, T]    int32  as for the attention, but a node without a parent is never reached (but node
+ *                            0).  NULL: a chain
+ *   u       [B, T]    fp32   random numbers in [0, 1)  (NaN and below: 0; above: the largest below 1)
+ *   lengths [B]       int32  nodes n_b, at most T of which count; NULL: T.  0: path is empty, next = -1
+ *   path    [B, T]    int32  output: node 0 and the accepted nodes, ascending, -1 padded
+ *   count   [B]       int32  output: their number
+ *   next    [B]       int32  output: the token that follows
+ * Supported: 1 <= T <= 64, 1 <= V <= 2^19.  Workspace: gca_verify_workspace_size(B, T, V) bytes,
+ * 256-byte aligned. */
+gca_status gca_verify(int64_t B, int64_t T, int64_t V, const float* p, const float* q, const int32_t* tokens,
+                      const int32_t* parents, const float* u, const int32_t* lengths, int32_t* path, int32_t* count,
+                      int32_t* next, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Bytes of gca_verify's workspace; 0 if the sizes are invalid. */
+size_t gca_verify_workspace_size(int64_t B, int64_t T, int64_t V);
+
 /* Profiling aid (outside the method).  While armed, the i-th kernel that libgca
  * launches from the calling thread (i = 0, 1, ... while 2 (i + 1) <= capacity,
  * capacity <= 4096) is dispatched with events[2 i] and events[2 i + 1] as its

@@ -12,6 +12,7 @@
 #include "cache_plan.hpp"
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
+#include "numbers8.hpp"
 
 namespace gca {
 namespace {
@@ -54,46 +55,6 @@ __device__ __forceinline__ uint32_t max_u64(uint32_t x) {
   x = max(a, b);
   pair32(x, a, b);
   return max(a, b);
-}
-
-// One row's 8 entries of a lane.
-template <typename T> struct Row8;
-template <> struct Row8<__bf16> {
-  u32x4 x;  // pairs of bf16
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t src, uint32_t at, int row) {
-    x = __builtin_amdgcn_raw_buffer_load_b128(src, at, row, 0);
-  }
-  __device__ __forceinline__ float at(int c) const {
-    const uint32_t w = x[c >> 1];
-    return __uint_as_float((c & 1) ? (w & 0xffff0000u) : (w << 16));
-  }
-};
-template <> struct Row8<float> {
-  f32x4 lo, hi;
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t src, uint32_t at, int row) {
-    lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(src, at, row, 0));
-    hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(src, at + 16, row, 0));
-  }
-  __device__ __forceinline__ float at(int c) const { return c < 4 ? lo[c] : hi[c - 4]; }
-};
-
-// 8 x 8 bytes, row r in (x[2 r], x[2 r + 1]), transposed in place: four 4 x 4 blocks, each
-// turned by two levels of byte permutes.
-__device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t& o0, uint32_t& o1,
-                                           uint32_t& o2, uint32_t& o3) {
-  // v_perm_b32(hi, lo, sel): selector 0-3 takes a byte of lo, 4-7 of hi
-  const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602);
-  const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602);
-  o0 = __builtin_amdgcn_perm(cd0, ab0, 0x05040100);
-  o1 = __builtin_amdgcn_perm(cd0, ab0, 0x07060302);
-  o2 = __builtin_amdgcn_perm(cd1, ab1, 0x05040100);
-  o3 = __builtin_amdgcn_perm(cd1, ab1, 0x07060302);
-}
-
-// Two numbers to e4m3 (round to nearest even), into one half of w.
-__device__ __forceinline__ uint32_t pk_e4m3(float a, float b, uint32_t w, bool hi) {
-  return hi ? (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)w, true)
-            : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)w, false);
 }
 
 // Chunks with tokens among n, of a sequence of `total` new tokens.

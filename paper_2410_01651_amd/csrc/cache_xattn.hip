@@ -35,12 +35,10 @@
 #include "cache_plan.hpp"
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
+#include "numbers8.hpp"
 
 namespace gca {
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 
 constexpr int kMaxWaves = 8;
 constexpr int kTileBytes = kS * kD;
@@ -68,79 +66,6 @@ struct XattnParams {
   uint32_t negate;  // the sign bits of one query entry (fp32) or two, if attn_scale < 0
   int off_by_one;
 };
-
-__device__ __forceinline__ f32x16 mma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mma(const f16x8& a, const f16x8& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma(const f16x8& a, const f16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-
-// Eight numbers (dwords x, y) as a bf16 / fp16 operand, exactly.
-template <bool I8>
-__device__ __forceinline__ bf16x8 to_bf16(uint32_t x, uint32_t y) {
-  if constexpr (I8) {
-    bf16x8 f;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      f[m] = (__bf16)(float)(int8_t)((int)x >> (8 * m));
-      f[4 + m] = (__bf16)(float)(int8_t)((int)y >> (8 * m));
-    }
-    return f;
-  } else {
-    const u32x4 r = u32x4{
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false)),
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true)),
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.f, false)),
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.f, true))};
-    return __builtin_bit_cast(bf16x8, r);
-  }
-}
-template <bool I8>
-__device__ __forceinline__ f16x8 to_f16(uint32_t x, uint32_t y) {
-  if constexpr (I8) {
-    // n + 128 in the low mantissa bits of 1024: fp16 1152 + n
-    auto two = [](uint32_t u, uint32_t sel) {
-      const f16x2 m = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, sel));
-      return __builtin_bit_cast(uint32_t, m - f16x2{(_Float16)1152, (_Float16)1152});
-    };
-    x ^= 0x80808080u;
-    y ^= 0x80808080u;
-    return __builtin_bit_cast(
-        f16x8, u32x4{two(x, 0x04010400), two(x, 0x04030402), two(y, 0x04010400), two(y, 0x04030402)});
-  } else {
-    const u32x4 r = u32x4{
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, false)),
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true)),
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y, 1.f, false)),
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y, 1.f, true))};
-    return __builtin_bit_cast(f16x8, r);
-  }
-}
-
-__device__ __forceinline__ void store8(__bf16* p, const float* x) {
-  bf16x8 r;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (__bf16)x[e];
-  *reinterpret_cast<bf16x8*>(p) = r;
-}
-__device__ __forceinline__ void store8(float* p, const float* x) {
-  reinterpret_cast<f32x4*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-  reinterpret_cast<f32x4*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
-}
-
-// A wave-uniform address in scalar registers.  (As a pointer to global memory: through an integer it would
-// lose that, and a wait for a load that might be from elsewhere is a wait for all loads.)
-template <typename T>
-__device__ __forceinline__ __attribute__((address_space(1))) T* scalar_ptr(T* x) {
-  return reinterpret_cast<__attribute__((address_space(1))) T*>(uniform_addr(x));
-}
 
 // (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
 // floating point flags and would be called.)

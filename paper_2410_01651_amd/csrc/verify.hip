@@ -1,0 +1,359 @@
+// Verification of drafted tokens (gca_verify): a walk down each sequence's tree by rejection sampling, and
+// the draw of the token that follows.
+//
+// Mathematics.  At node a, with r = p[a] and z = 1, child x is accepted with probability
+// min(1, r[x] / (z q[x])); a rejection leaves r <- max(r - z q, 0), z <- sum r.  (r / z is then the
+// distribution that the next child, drawn from q too, has to make up for; with the draw from r at
+// the end each token comes out with probability p[a].)  Children that were chosen rather than drawn are q = 1
+// at x.  Everything is fp64 without contraction, and sums are of whole multiples of 2^-44 in 64-bit integers
+// (2^19 entries of at most 1 stay below 2^63), so that results do not depend on how the work is cut.
+//
+// Work.  One lane per node holds the node's token and its entries of p and q, so that the walk is
+// comparisons and ballots after two dependent loads.  The vocabulary is cut into slices, one
+// workgroup each, and each workgroup repeats the walk rather than wait for another's; only a rejected child
+// that was drawn from q and has a sibling left needs the sum over the whole vocabulary on the way, which every
+// workgroup then forms by itself.  A second launch picks the slice and the token by the slices' sums.
+// Bound by HBM, the last node's p (and q, where it was rejected from), or, for few sequences, by
+// the trips to memory.
+#include "gca_device.hpp"
+#include "gca_launch.hpp"
+#include "window_plan.hpp"
+
+namespace gca {
+namespace {
+
+constexpr int kVerifyThreads = 256;
+constexpr int kVerifyWaves = kVerifyThreads / 64;
+constexpr double kFix = 17592186044416.0;       // 2^44
+constexpr double kUnfix = 1.0 / 17592186044416.0;
+
+// What a walk ends with, per sequence.
+struct Walk {
+  int32_t node;      // the last node, -1: no nodes
+  int32_t rejected;  // children rejected there
+  uint64_t on;       // the walk's nodes
+  double z[kTreeNodes];      // drawn children: z before each rejection
+  int32_t token[kTreeNodes]; // chosen ones: the rejected tokens
+};
+
+struct VerifyParams {
+  const float* p;
+  const float* q;
+  const int32_t* tokens;
+  const int32_t* parents;
+  const float* u;
+  const int32_t* lengths;
+  int32_t* path;
+  int32_t* count;
+  int32_t* next;
+  Walk* walk;      // [B]
+  int64_t* sums;   // [B][slices]
+  uint32_t B, T, slices;
+  uint32_t V, per;  // entries in all, and per slice (a multiple of 4)
+};
+
+// A probability as it counts.
+__device__ __forceinline__ double prob(float x) {
+  return x > 0.f ? (double)fminf(x, 1.f) : 0.0;  // (NaN and below: 0)
+}
+// r - z q, at least 0: a product and a difference, each rounded.
+__device__ __forceinline__ double less(double r, double z, double q) {
+#pragma clang fp contract(off)
+  const double s = z * q;
+  const double d = r - s;
+  return d > 0.0 ? d : 0.0;
+}
+// r in whole multiples of 2^-44, to the nearest (ties to even): 0 .. 2^44, so the sum with 2^52 holds it
+// in its mantissa.
+__device__ __forceinline__ int64_t whole(double r) {
+  const double x = r * kFix + 4503599627370496.0;
+  return __double_as_longlong(x) & 0xfffffffffffffll;
+}
+
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) x += __shfl_xor(x, s);
+  return x;
+}
+
+// r[x] of the walk's last node.
+__device__ __forceinline__ double left(const Walk& w, bool drawn, float p, float q, uint32_t x) {
+  double r = prob(p);
+  if (drawn) {
+    const double c = prob(q);
+    for (int j = 0; j < w.rejected; ++j) r = less(r, w.z[j], c);
+  } else {
+    for (int j = 0; j < w.rejected; ++j)
+      if (w.token[j] == (int32_t)x) r = 0.0;
+  }
+  return r;
+}
+
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4u;
+
+// This thread's part of the sum of r over entries [lo, hi) of the last node's row; `plain`: of p[a] itself.
+__device__ __forceinline__ int64_t part_sum(const VerifyParams& p, const Walk& w, uint32_t b, uint32_t lo, uint32_t hi,
+                                            bool plain) {
+  const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
+  const float* pr = p.p + row;
+  const bool drawn = p.q != nullptr, with_q = drawn && w.rejected > 0 && !plain;
+  const float* qr = with_q ? p.q + row : pr;
+  int64_t sum = 0;
+  for (uint32_t x = lo + 4 * threadIdx.x; x < hi; x += 4 * kVerifyThreads) {
+    if (x + 4 <= hi) {
+      const f32x4u a = *reinterpret_cast<const f32x4u*>(pr + x), c = *reinterpret_cast<const f32x4u*>(qr + x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += whole(plain ? prob(a[e]) : left(w, drawn, a[e], c[e], x + e));
+    } else {
+      for (uint32_t y = x; y < hi; ++y) sum += whole(plain ? prob(pr[y]) : left(w, drawn, pr[y], qr[y], y));
+    }
+  }
+  return sum;
+}
+
+// Sum over the workgroup, to every thread.
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* lds) {
+  x = wave_sum(x);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  int64_t s = 0;
+#pragma unroll
+  for (int w = 0; w < kVerifyWaves; ++w) s += lds[w];
+  return s;
+}
+
+__global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParams p) {
+  __shared__ Walk w;
+  __shared__ int64_t lds[kVerifyWaves];
+  __shared__ int again;
+  const uint32_t b = blockIdx.x / p.slices, slice = blockIdx.x - b * p.slices;
+  const int lane = threadIdx.x & 63;
+  const bool first_wave = threadIdx.x < 64, drawn = p.q != nullptr;
+
+  // lane i: node i
+  int n = p.lengths ? p.lengths[b] : (int)p.T;
+  n = max(min(n, (int)p.T), 0);
+  int par = -1, tok = -1;
+  float u = 0.f;
+  double r = 0.0, q = 0.0;
+  bool real = false;  // a token of the vocabulary
+  if (first_wave && lane < n) {
+    const int64_t at = (int64_t)b * p.T + lane;
+    par = p.parents ? p.parents[at] : lane - 1;
+    if (par >= lane) par = -1;
+    tok = p.tokens[at];
+    u = p.u[at];
+    u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+    real = par >= 0 && tok >= 0 && (uint32_t)tok < p.V;
+    if (real) {
+      const int64_t e = ((int64_t)b * p.T + par) * p.V + tok;
+      r = prob(p.p[e]);
+      q = drawn ? prob(p.q[e]) : 1.0;
+    }
+  }
+  int cur = n > 0 ? 0 : -1, rejected = 0;
+  uint64_t on = n > 0 ? 1 : 0, done = 0;  // accepted nodes; tested ones
+  double z = 1.0;
+  for (;;) {
+    if (first_wave) {
+      again = 0;
+      for (;;) {
+        const uint64_t open = cur < 0 ? 0 : __ballot(lane < n && par == cur) & ~done;
+        if (open == 0) break;
+        const int c = __builtin_ctzll(open);
+        done |= 1ull << c;
+        const double rc = __shfl(r, c), qc = __shfl(q, c);
+        const double uc = (double)__shfl(u, c);
+        const int tc = __shfl(tok, c);
+        if (!__shfl((int)real, c)) continue;
+        bool take;
+        {
+#pragma clang fp contract(off)
+          const double s = z * qc;
+          const double us = uc * s;
+          take = us < rc;
+        }
+        if (take) {
+          cur = c;
+          on |= 1ull << c;
+          rejected = 0;
+          z = 1.0;
+          continue;
+        }
+        if (drawn) {
+          if (lane == 0) w.z[rejected] = z;
+          ++rejected;
+          if (par == cur) r = less(r, z, q);
+          if ((open & (open - 1)) != 0) {  // a sibling is left: its test needs the sum
+            again = 1;
+            break;
+          }
+        } else {
+          if (lane == 0) w.token[rejected] = tc;
+          ++rejected;
+          const double d = z - rc;
+          z = d > 0.0 ? d : 0.0;
+          if (par == cur && tok == tc) r = 0.0;
+        }
+      }
+      if (lane == 0) {
+        w.node = cur;
+        w.rejected = rejected;
+        w.on = on;
+      }
+    }
+    __syncthreads();
+    if (!again) break;
+    const int64_t s = block_sum(part_sum(p, w, b, 0, p.V, false), lds);
+    z = (double)s * kUnfix;
+    __syncthreads();  // (`again` and the walk are read before they are written again)
+  }
+
+  if (slice == 0) {
+    if (first_wave && lane < (int)p.T) {  // entry i of the path is the i-th node of the walk
+      const int64_t at = (int64_t)b * p.T;
+      const int count = __builtin_popcountll(on);
+      if (on >> lane & 1) p.path[at + __builtin_popcountll(on & ((1ull << lane) - 1))] = lane;
+      if (lane >= count) p.path[at + lane] = -1;
+      if (lane == 0) p.count[b] = count;
+    }
+    const int words = sizeof(Walk) / 4;
+    for (int x = threadIdx.x; x < words; x += kVerifyThreads)
+      reinterpret_cast<uint32_t*>(p.walk + b)[x] = reinterpret_cast<const uint32_t*>(&w)[x];
+  }
+  if (w.node < 0) return;
+  const uint32_t lo = slice * p.per, hi = min(lo + p.per, p.V);
+  const int64_t s = block_sum(part_sum(p, w, b, lo, hi, false), lds);
+  if (threadIdx.x == 0) p.sums[(int64_t)b * p.slices + slice] = s;
+}
+
+// One workgroup per sequence: the slice that the drawn place is in, and the token in it.
+__global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParams p) {
+  __shared__ Walk w;
+  __shared__ int64_t lds[kVerifyWaves];
+  __shared__ int64_t place;  // in the slice
+  __shared__ uint32_t chosen;
+  const uint32_t b = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int x = tid; x < (int)(sizeof(Walk) / 4); x += kVerifyThreads)
+    reinterpret_cast<uint32_t*>(&w)[x] = reinterpret_cast<const uint32_t*>(p.walk + b)[x];
+  float u = p.u[(int64_t)b * p.T];
+  u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+  __syncthreads();
+  if (w.node < 0) {
+    if (tid == 0) p.next[b] = -1;
+    return;
+  }
+  const bool drawn = p.q != nullptr;
+  // (one slice per thread: at most kVerifyThreads of them)
+  int64_t mine = tid < (int)p.slices ? p.sums[(int64_t)b * p.slices + tid] : 0;
+  bool plain = false;
+  int64_t total = block_sum(mine, lds);
+  uint32_t lo = 0, hi = p.V;
+  if (total == 0) {  // nothing is left: of p itself, the whole vocabulary as one slice
+    plain = true;
+    total = block_sum(part_sum(p, w, b, 0, p.V, true), lds);
+    if (total == 0) {
+      if (tid == 0) p.next[b] = -1;
+      return;
+    }
+    if (tid == 0) place = (int64_t)((double)u * (double)total);
+    __syncthreads();
+  } else {
+    const int64_t at = (int64_t)((double)u * (double)total);
+    int64_t upto = mine;  // sum of the slices up to this one
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const int64_t y = __shfl_up(upto, s);
+      if (lane >= s) upto += y;
+    }
+    __syncthreads();
+    if (lane == 63) lds[tid >> 6] = upto;
+    __syncthreads();
+    for (int y = 0; y < (tid >> 6); ++y) upto += lds[y];
+    if (upto > at && upto - mine <= at) {  // one thread
+      chosen = tid;
+      place = at - (upto - mine);
+    }
+    __syncthreads();
+    lo = chosen * p.per;
+    hi = min(lo + p.per, p.V);
+  }
+  // blocks of entries in order, one per thread and step
+  const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
+  const float* pr = p.p + row;
+  const float* qr = drawn && w.rejected > 0 ? p.q + row : pr;
+  int64_t before = 0;
+  for (uint32_t x0 = lo; x0 < hi; x0 += kVerifyThreads) {
+    const uint32_t x = x0 + tid;
+    const int64_t r = x < hi ? whole(plain ? prob(pr[x]) : left(w, drawn, pr[x], qr[x], x)) : 0;
+    int64_t upto = r;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const int64_t y = __shfl_up(upto, s);
+      if (lane >= s) upto += y;
+    }
+    __syncthreads();
+    if (lane == 63) lds[tid >> 6] = upto;
+    __syncthreads();
+    int64_t step = 0;
+    for (int y = 0; y < kVerifyWaves; ++y) {
+      if (y < (tid >> 6)) upto += lds[y];
+      step += lds[y];
+    }
+    upto += before;
+    if (upto > place && upto - r <= place) p.next[b] = (int32_t)x;
+    before += step;
+    if (before > place) break;  // (uniform)
+  }
+}
+
+}  // namespace
+
+VerifyPlan verify_plan(int64_t B, int64_t V) {
+  // slices of a few thousand entries, as many as fill the chip four workgroups per CU
+  int64_t slices = (V + 4095) / 4096;
+  const int64_t fill = 4 * (int64_t)device_cus();
+  if (slices * B > fill) slices = fill / B;
+  if (slices > kVerifyThreads) slices = kVerifyThreads;
+  if (slices < 1) slices = 1;
+  VerifyPlan a;
+  a.per = ((V + slices - 1) / slices + 3) / 4 * 4;
+  a.slices = (V + a.per - 1) / a.per;
+  return a;
+}
+
+size_t verify_workspace(int64_t B, int64_t T, int64_t V) {
+  (void)T;
+  return align256((size_t)B * sizeof(Walk)) + align256((size_t)B * verify_plan(B, V).slices * sizeof(int64_t));
+}
+
+hipError_t launch_verify(int64_t B, int64_t T, int64_t V, const float* p, const float* q, const int32_t* tokens,
+                         const int32_t* parents, const float* u, const int32_t* lengths, int32_t* path, int32_t* count,
+                         int32_t* next, void* ws, hipStream_t stream) {
+  const VerifyPlan a = verify_plan(B, V);
+  VerifyParams k;
+  k.p = p;
+  k.q = q;
+  k.tokens = tokens;
+  k.parents = parents;
+  k.u = u;
+  k.lengths = lengths;
+  k.path = path;
+  k.count = count;
+  k.next = next;
+  k.walk = static_cast<Walk*>(ws);
+  k.sums = reinterpret_cast<int64_t*>(static_cast<char*>(ws) + align256((size_t)B * sizeof(Walk)));
+  k.B = (uint32_t)B;
+  k.T = (uint32_t)T;
+  k.slices = (uint32_t)a.slices;
+  k.V = (uint32_t)V;
+  k.per = (uint32_t)a.per;
+  launch_kernel("verify_walk_kernel", verify_walk_kernel, dim3((unsigned)(B * a.slices)), dim3(kVerifyThreads), 0,
+                stream, k);
+  launch_kernel("verify_draw_kernel", verify_draw_kernel, dim3((unsigned)B), dim3(kVerifyThreads), 0, stream, k);
+  return take_launch_error();
+}
+
+}  // namespace gca

@@ -1,0 +1,675 @@
+// Attention of the newest tokens over the 8-bit token window (gca_window_attn): single tokens, trees of
+// drafted tokens, and prompts.
+//
+// Mathematics.  K_p = kappa_p N_p and V_p = nu_p M_p with 8-bit numbers N, M and one scale per token.  One
+// pass over the tiles of 64 positions that a block of rows sees, with each row's running maximum m and sum
+// l:  s = attn_scale kappa_p q N_p^T + slope (p - pos), P = exp(s - m), and out = sum P nu M / l.
+// Every e4m3 number and every int8 is exact in bf16 and in fp16.  An e4m3 key takes its scale (a power of
+// two) along in the conversion; int8 scores are multiplied by theirs.  So q N^T is a product of exact
+// operands with fp32 sums (fp32 queries: three bf16 terms, 24 bits), and P nu / u meets M in fp16,
+// 11 bits (fp32 tensors: two fp16 terms, 22 bits), u being a power of two by the largest nu that the block of
+// rows has met so far: P <= 1, so fp16 holds the product, and when a tile brings a larger nu what was
+// summed is rescaled with the same factor that a new maximum brings.
+//
+// Layout.  As in the chunk cache's attention: S^T = N Q^T and O^T = M^T P^T on MFMA tiles of W x W, lane
+// l = W g + c having query row c as its column, the rows of N in the order that makes a lane's
+// accumulators consecutive tokens, so that P is the second product's operand as it stands, and a tile is
+// 4 loads of 16 bytes per lane straight into registers.  Scales come one token per lane and are
+// handed round through 512 bytes of LDS per wave.
+//
+// Work.  One item per (sequence, cached head, block of rows); its waves, of one or more workgroups, take the
+// tiles in turn and leave (m, l, out) to be joined.
+#include "gca_device.hpp"
+#include "gca_launch.hpp"
+#include "numbers8.hpp"
+#include "window_plan.hpp"
+
+namespace gca {
+namespace {
+
+constexpr int kMaxWaves = 8;
+constexpr int kTileBytes = kS * kD;
+constexpr float kLowest = -3.402823466e38f;  // of a row that has seen nothing
+
+struct WindowParams {
+  uint32_t items;           // workgroups with work
+  uint32_t splits, blocks;  // workgroups per row block; row blocks per (sequence, cached head)
+  uint32_t nw;              // waves per workgroup
+  uint32_t Hkv, G, T, M;    // M = G T: query rows of a group
+  uint32_t per_head;        // row blocks per head; 0: the group's rows are one list
+  uint32_t H;
+  uint32_t ring_tiles;      // capacity / 64
+  int32_t ring, window;
+  const int32_t* length;
+  const int32_t* parents;
+  const int32_t* lengths;
+  const float* slopes;
+  const uint8_t* k;
+  const uint8_t* v;
+  const float* ks;
+  const float* vs;
+  const void* q;
+  void* out;
+  float* lse;
+  float* part;    // partial results of split row blocks: [item][row][64], then [item][row][2]
+  float* part_ml;
+  float scale;    // |attn_scale| log2 e (log2 e where attn_scale is 0)
+  float unscale;  // 1 / |attn_scale| (1)
+  uint32_t negate, keep;  // xor and and masks of one query entry (fp32) or two: the scale's sign, and zero
+  int off_by_one;
+};
+
+// out = sum_w exp2(m_w - m) o_w / (sum_w exp2(m_w - m) l_w), and the row's log-sum-exp.
+struct Joined {
+  float m, l;
+};
+__device__ __forceinline__ Joined finish(float m, float l, int off_by_one) {
+  if (off_by_one) {
+    const float top = fmaxf(m, 0.f);
+    l = l * __builtin_amdgcn_exp2f(m - top) + __builtin_amdgcn_exp2f(-top);
+    m = top;
+  }
+  return Joined{m, l};
+}
+
+// (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
+// floating point flags and would be called.)
+// T: type of the queries; W: MFMA tile; NC: column blocks of W query rows.
+template <typename T, bool I8, int W, int NC>
+__global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowParams p) {
+  constexpr bool kB16 = sizeof(T) == 2;
+  constexpr int NG = 64 / W;           // lane groups
+  constexpr int NA = 64 / W;           // blocks of W tokens (or columns) per tile
+  constexpr int NK = W / 8;            // steps of the contraction over 64 columns (or tokens)
+  constexpr int NX = NK / 2;           // 16-byte pieces per lane and block
+  constexpr int NR = W * W / 64;       // accumulators per block
+  constexpr int NV = NA * NR;          // values per lane and column block
+  constexpr int QP = kB16 ? 1 : 3;     // bf16 terms of a query entry
+  constexpr int PP = kB16 ? 1 : 2;     // fp16 terms of a probability
+  constexpr int QB = W * NC;           // query rows per item
+  typedef __attribute__((ext_vector_type(NR))) float Acc;
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+
+  const uint32_t it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
+  if (it >= p.items) return;
+  const uint32_t tid = __builtin_amdgcn_workitem_id_x(), nw = p.nw;
+  const int lane = tid & 63, g = lane / W, col = lane % W;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
+  // item = ((b Hkv + h) blocks + block) splits + split
+  const uint32_t bb = scalar(it / p.splits), split = it - bb * p.splits;
+  const uint32_t bh = scalar(bb / p.blocks), blk = bb - bh * p.blocks;
+  const uint32_t b = scalar(bh / p.Hkv), h = bh - b * p.Hkv;
+
+  // ---- the block's rows [m0, m0 + nrows) of the group's M, and the new tokens they belong to
+  uint32_t m0, nrows, tmin, tmax;
+  if (p.per_head) {
+    const uint32_t gh = scalar(blk / p.per_head);
+    tmin = (blk - gh * p.per_head) * QB;
+    nrows = min((uint32_t)QB, p.T - tmin);
+    tmax = tmin + nrows - 1;
+    m0 = gh * p.T + tmin;
+  } else {
+    m0 = blk * QB;
+    nrows = min((uint32_t)QB, p.M - m0);
+    const uint32_t f = scalar(m0 / p.T), l = scalar((m0 + nrows - 1) / p.T);
+    tmin = f == l ? m0 - f * p.T : 0;
+    tmax = f == l ? tmin + nrows - 1 : p.T - 1;
+  }
+  const int length = max((int)scalar((uint32_t)p.length[b]), 0);
+  int n = p.lengths ? (int)scalar((uint32_t)p.lengths[b]) : (int)p.T;
+  n = max(min(n, (int)p.T), 0);
+  const int base = length - n;  // (negative only if fewer tokens were appended than `lengths` says)
+
+  // ---- the tree: lane i holds node i's ancestors and itself as bits
+  uint64_t up = 0;
+  if (p.parents) {
+    const int i = lane;
+    int par = p.parents[(int64_t)b * p.T + min((uint32_t)i, p.T - 1)];
+    par = par >= 0 && par < i ? par : i;
+    uint32_t lo = i < 32 ? 1u << i : 0u, hi = i < 32 ? 0u : 1u << (i - 32);
+#pragma unroll
+    for (int s = 0; s < 6; ++s) {  // 2^s levels at a time
+      lo |= (uint32_t)__builtin_amdgcn_ds_bpermute(4 * par, (int)lo);
+      hi |= (uint32_t)__builtin_amdgcn_ds_bpermute(4 * par, (int)hi);
+      par = __builtin_amdgcn_ds_bpermute(4 * par, par);
+    }
+    up = (uint64_t)hi << 32 | lo;
+  }
+
+  // ---- this lane's rows
+  uint32_t row[NC];    // of the group
+  int depth[NC];       // position - base
+  uint64_t sees[NC];   // tree: new tokens it sees
+  uint64_t above[NC];  // tree: its ancestors and itself
+  float slope[NC];     // in units of a score before its scale
+  bool live[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const uint32_t m = m0 + min((uint32_t)(c * W + col), nrows - 1);
+    const uint32_t gh = m / p.T, t = m - gh * p.T;
+    row[c] = m;
+    depth[c] = (int)t;
+    live[c] = (uint32_t)(c * W + col) < nrows && (int)t < n;
+    above[c] = sees[c] = 0;
+    if (p.parents) {
+      const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (int)t, (int)(uint32_t)up);
+      const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (int)t, (int)(uint32_t)(up >> 32));
+      above[c] = (uint64_t)hi << 32 | lo;
+      depth[c] = __builtin_popcountll(above[c]) - 1;
+      sees[c] = above[c];
+      if (p.window)  // ancestors `window` levels up or more
+        for (int x = depth[c] - p.window; x >= 0; --x) sees[c] &= sees[c] - 1;
+    }
+    slope[c] = p.slopes ? p.slopes[h * p.G + gh] * p.unscale : 0.f;
+  }
+
+  // ---- tiles of 64 positions that the rows see: [t0, t1)
+  const int dmin = p.parents ? 0 : (int)tmin, dmax = p.parents ? kTreeNodes - 1 : (int)tmax;
+  const int first = p.window ? max(base + dmin - p.window + 1, 0) : 0;
+  const int last = p.parents ? length - 1 : min(base + (int)tmax, length - 1);  // position
+  const int t0 = first >> 6;
+  int t1 = (last >> 6) + 1;
+  if (!p.ring) t1 = min(t1, (int)p.ring_tiles);
+  if ((int)tmin >= n) t1 = t0;
+  // every row sees the whole of a tile within [full0, full1]
+  const int full0 = p.window ? base + dmax - p.window + 1 : 0;
+  const int full1 = p.parents ? base - 1 : base + (int)tmin;
+  const uint32_t workers = p.splits * nw, me = split * nw + wave;
+
+  const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
+                                    : 16 * (col >> 2) + (col & 3);
+  const uint32_t lane_off = lane_row * kD + 16 * g;
+  const int64_t head_tiles = (int64_t)bh * p.ring_tiles;
+  // (`there` false: nothing is wanted and the descriptor is empty; the loads are issued either way, so that
+  // what is in flight at a wait is known)
+  auto slot = [&](int t) { return p.ring ? scalar((uint32_t)t % p.ring_tiles) : (uint32_t)t; };
+  auto load_tile = [&](u32x4* x, const uint8_t* from, uint32_t s, bool there) {
+    const __amdgpu_buffer_rsrc_t tile =
+        range_rsrc(reinterpret_cast<const char*>(from) + (head_tiles + s) * kTileBytes, there ? kTileBytes : 0);
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+        x[a * NX + y] = __builtin_amdgcn_raw_buffer_load_b128(
+            tile, lane_off, (W == 32 ? 32 : 4) * a * kD + 16 * NG * y, 0);
+  };
+  auto load_scale = [&](const float* from, uint32_t s, bool there) {
+    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+        range_rsrc(reinterpret_cast<const char*>(from + (head_tiles + s) * kS), there ? kS * 4 : 0), lane * 4, 0, 0));
+  };
+
+  int t = t0 + (int)me;
+  u32x4 kr[NA * NX], vr[NA * NX];
+  float ksc, vsc;
+  {
+    const bool there = t < t1;
+    const uint32_t s = there ? slot(t) : 0;
+    load_tile(kr, p.k, s, there);
+    ksc = load_scale(p.ks, s, there);
+    vsc = load_scale(p.vs, s, there);
+    load_tile(vr, p.v, s, there);
+  }
+
+  // ---- the queries: lane (g, c) takes columns 16 (g + NG x) .. of row c, x < NX
+  const int64_t row0 = (int64_t)(b * p.H + h * p.G) * p.T;
+  bf16x8 qf[NC][NK][QP];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const auto* qr = scalar_ptr(reinterpret_cast<const T*>(p.q) + row0 * kD) + (int64_t)row[c] * kD;
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      const auto* src = qr + 16 * (g + NG * (s >> 1)) + 8 * (s & 1);
+      if constexpr (kB16) {
+        u32x4 x = *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(src);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (x[e] ^ p.negate) & p.keep;
+        qf[c][s][0] = __builtin_bit_cast(bf16x8, x);
+      } else {
+#pragma unroll
+        for (int m8 = 0; m8 < 8; ++m8) {
+          float x = src[m8];
+          x = __uint_as_float((__float_as_uint(x) ^ p.negate) & p.keep);
+#pragma unroll
+          for (int e = 0; e < QP; ++e) {
+            const __bf16 part = (__bf16)x;
+            qf[c][s][e][m8] = part;
+            x -= (float)part;
+          }
+        }
+      }
+    }
+  }
+
+  float* const sc_lds = smem + wave * 128;  // this wave's scales: 64 of keys, 64 of values
+  Acc o[NC][NA];
+  float mx[NC], sum[NC];
+  int octave = -1000;  // of u
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    mx[c] = kLowest;
+    sum[c] = 0.f;
+#pragma unroll
+    for (int a = 0; a < NA; ++a) o[c][a] = Acc{};
+  }
+
+  for (; t < t1; t += (int)workers) {
+    const int p0 = t << 6;  // the tile's first position
+    const int tn = t + (int)workers;
+    const bool more = tn < t1;
+    const uint32_t sn = more ? slot(tn) : 0;
+
+    // scales, those of values over u: tokens that nobody sees have none
+    const int from = first - p0, to = length - p0;  // what may be seen of the tile
+    const bool here = lane >= from && lane < to;
+    const float nu = here ? vsc : 0.f;
+    const float big = max64(nu);
+    int up_by = 0;  // octaves that u grows by
+    if (big > 0.f) {
+      const int e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(big));
+      if (e > octave) {
+        up_by = octave == -1000 ? 0 : e - octave;
+        octave = e;
+      }
+    }
+    wave_lds_order();
+    sc_lds[lane] = ksc;
+    sc_lds[64 + lane] = __builtin_ldexpf(nu, 15 - octave);  // at most 2^15
+    wave_lds_order();
+
+    // S^T = N Q^T
+    Acc st[NC][NA];
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) st[c][a] = Acc{};
+      float kappa = 1.f;
+      if constexpr (!I8) kappa = sc_lds[lane_row + (W == 32 ? 32 : 4) * a];
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const u32x4 r = kr[a * NX + (i >> 1)];
+        bf16x8 f;
+        if constexpr (I8) f = to_bf16<true>(r[2 * (i & 1)], r[2 * (i & 1) + 1]);
+        else f = to_bf16_times(r[2 * (i & 1)], r[2 * (i & 1) + 1], kappa);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < QP; ++e) st[c][a] = mma(f, qf[c][i][e], st[c][a]);
+      }
+    }
+    load_tile(kr, p.k, sn, more);
+    ksc = load_scale(p.ks, sn, more);
+    vsc = load_scale(p.vs, sn, more);
+
+    const bool masked = p0 < full0 || p0 + kS - 1 > full1;
+    f16x8 pf[NC][NK][PP];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float v[NV];
+#pragma unroll
+      for (int u = 0; u < NV; ++u) v[u] = st[c][u / NR][u % NR];
+      // value u is token tok(u) + 16 g of the tile
+      auto tok = [](int u) { return W == 32 ? 32 * (u / 16) + u % 16 : u; };
+      if constexpr (I8) {
+#pragma unroll
+        for (int u = 0; u < NV; u += 4) {
+          const f32x4 s4 = *reinterpret_cast<const f32x4*>(sc_lds + 16 * g + tok(u));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[u + e] *= s4[e];
+        }
+      }
+      uint64_t mask = ~0ull;
+      if (masked) {
+        const int off = base - p0;  // the first new token
+        const int lo = p.window ? max(base + depth[c] - p.window + 1 - p0, 0) : 0;
+        if (p.parents) {
+          mask = off >= 64 ? ~0ull : off > 0 ? (1ull << off) - 1 : 0ull;
+          mask = lo < 64 ? mask & (~0ull << lo) : 0ull;
+          if (off < 64) mask |= off >= 0 ? sees[c] << off : off > -64 ? sees[c] >> -off : 0ull;
+        } else {
+          const int hi = off + depth[c];  // the row's own
+          mask = lo < 64 && hi >= 0 ? (~0ull << lo) & (hi < 63 ? (2ull << hi) - 1 : ~0ull) : 0ull;
+        }
+        if (to < 64) mask &= to > 0 ? (1ull << to) - 1 : 0ull;
+      }
+      if (p.slopes) {
+        // relative to the tile's first token; its own place joins the maximum below
+#pragma unroll
+        for (int u = 0; u < NV; ++u) v[u] = fmaf(slope[c], (float)tok(u), v[u]);
+        if (p.parents && p0 + kS > base) {  // a node's position is its depth's, not its place's
+#pragma unroll
+          for (int u = 0; u < NV; ++u) {
+            const int a = p0 + 16 * g + tok(u) - base;
+            if (a > 0 && a < 64) {
+              const int d = __builtin_popcountll(above[c] & ((1ull << a) - 1));
+              v[u] = fmaf(slope[c], (float)(d - a), v[u]);
+            }
+          }
+        }
+      }
+      if (masked) {
+        const uint64_t mg = mask >> (16 * g);
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+          if (!(mg >> tok(u) & 1)) v[u] = -INFINITY;
+      }
+      float top = fmaxf(fmaxf(v[0], v[1]), v[2]), top2 = fmaxf(fmaxf(v[3], v[4]), v[5]);
+#pragma unroll
+      for (int u = 6; u + 3 < NV; u += 4) {
+        top = fmaxf(fmaxf(top, v[u]), v[u + 1]);
+        top2 = fmaxf(fmaxf(top2, v[u + 2]), v[u + 3]);
+      }
+      top = fmaxf(fmaxf(top, v[NV - 2]), fmaxf(top2, v[NV - 1]));
+      // where this lane's tokens begin, from the row
+      const float at = slope[c] * (float)(p0 + 16 * g - base - depth[c]);
+      top += at;
+      if constexpr (W == 16) {
+        uint32_t x, y;
+        pair16(__float_as_uint(top), x, y);
+        top = fmaxf(__uint_as_float(x), __uint_as_float(y));
+      }
+      top = fmaxf(max_xor32(top) * p.scale, mx[c]);
+      const float shrink = __builtin_amdgcn_exp2f(mx[c] - top);
+      mx[c] = top;
+      const float sub = at * p.scale - top;
+#pragma unroll
+      for (int u = 0; u < NV; ++u) v[u] = __builtin_amdgcn_exp2f(fmaf(v[u], p.scale, sub));
+      if (masked) {
+        const uint64_t mg = mask >> (16 * g);
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+          if (!(mg >> tok(u) & 1)) v[u] = 0.f;
+      }
+      float add = v[0], add2 = v[1];
+#pragma unroll
+      for (int u = 2; u < NV; u += 2) {
+        add += v[u];
+        add2 += v[u + 1];
+      }
+      sum[c] = fmaf(sum[c], shrink, add + add2);
+      const float both = up_by == 0 ? shrink : __builtin_ldexpf(shrink, -up_by);
+      if (__ballot(both != 1.f) != 0) {
+#pragma unroll
+        for (int a = 0; a < NA; ++a)
+#pragma unroll
+          for (int r = 0; r < NR; ++r) o[c][a][r] *= both;
+      }
+#pragma unroll
+      for (int u = 0; u < NV; u += 4) {
+        const f32x4 s4 = *reinterpret_cast<const f32x4*>(sc_lds + 64 + 16 * g + tok(u));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = v[u + e] * s4[e];
+          if constexpr (PP == 2) asm("" : "+v"(x));  // (one rounding of x for both terms)
+          const int i = (u + e) / 8, m = (u + e) % 8;
+          const _Float16 hi = (_Float16)x;
+          pf[c][i][0][m] = hi;
+          if constexpr (PP == 2) pf[c][i][PP - 1][m] = (_Float16)(x - (float)hi);
+        }
+      }
+      if (masked) {  // (a scale that is NaN stays with the rows that see it)
+        const uint64_t mg = mask >> (16 * g);
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+          if (!(mg >> tok(u) & 1))
+#pragma unroll
+            for (int e = 0; e < PP; ++e) pf[c][u / 8][e][u % 8] = (_Float16)0.f;
+      }
+    }
+
+    // O^T += M^T P^T (numbers behind the newest token are cleared: they may be anything)
+    if (to < kS) {
+      const int left0 = opaque(to - 16 * g);
+#pragma unroll
+      for (int y = 0; y < NX; ++y)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const int left = left0 - (16 * NG * y + 4 * d);
+          const uint32_t only = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+          for (int a = 0; a < NA; ++a) vr[a * NX + y][d] &= only;
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const u32x4 r = vr[a * NX + (i >> 1)];
+        const f16x8 f = to_f16<I8>(r[2 * (i & 1)], r[2 * (i & 1) + 1]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < PP; ++e) o[c][a] = mma(f, pf[c][i][e], o[c][a]);
+      }
+    load_tile(vr, p.v, sn, more);
+  }
+
+  // ---- output: value u of a lane is column 32 (u / 16) + 16 g + u % 16 (W = 32) or 16 g + u
+  const int back = octave == -1000 ? 0 : octave - 15;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {  // the groups' shares of the sums
+    if constexpr (W == 16) {
+      uint32_t x, y;
+      pair16(__float_as_uint(sum[c]), x, y);
+      sum[c] = __uint_as_float(x) + __uint_as_float(y);
+    }
+    sum[c] = sum_xor32(sum[c]);
+  }
+  T* const out0 = (T*)scalar_ptr(reinterpret_cast<T*>(p.out) + (row0 + m0) * kD);
+  if (workers == 1) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const uint32_t m = c * W + col;
+      if (m >= nrows) continue;
+      const Joined j = finish(mx[c], sum[c], p.off_by_one);
+      const bool none = !live[c] || sum[c] == 0.f;
+      // (off by one: the row's own scale between its maximum and the denominator's)
+      const float f = none ? 0.f : __builtin_amdgcn_exp2f(mx[c] - j.m) / j.l;
+      T* dst = out0 + m * kD + 16 * g;
+#pragma unroll
+      for (int u = 0; u < NV; u += 8) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          x[e] = none ? 0.f : __builtin_ldexpf(o[c][(u + e) / NR][(u + e) % NR] * f, back);
+        store8(dst + (u / 16) * 32 + u % 16, x);
+      }
+      if (p.lse && g == 0)
+        p.lse[row0 + m0 + m] = none ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+    }
+    return;
+  }
+  // the waves' parts: part[wave][row][16 blocks of 4], block x of row r at x ^ (r mod 16); then m and l
+  __syncthreads();
+  float* const part = smem;
+  float* const ml = smem + nw * nrows * kD;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const uint32_t m = c * W + col;
+    if (m >= nrows) continue;
+    float* pr = part + (wave * nrows + m) * kD;
+#pragma unroll
+    for (int u = 0; u < NV; u += 4) {
+      const Acc& a = o[c][u / NR];
+      const uint32_t x = (4 * g + (u / 16) * 8 + (u % 16) / 4) ^ (m & 15);
+      *reinterpret_cast<f32x4*>(pr + 4 * x) =
+          f32x4{__builtin_ldexpf(a[u % NR], back), __builtin_ldexpf(a[u % NR + 1], back),
+                __builtin_ldexpf(a[u % NR + 2], back), __builtin_ldexpf(a[u % NR + 3], back)};
+    }
+    if (g == 0) {
+      ml[2 * (wave * nrows + m)] = live[c] ? mx[c] : kLowest;
+      ml[2 * (wave * nrows + m) + 1] = live[c] ? sum[c] : 0.f;
+    }
+  }
+  __syncthreads();
+  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw) {
+    const uint32_t m = e >> 4, x = e & 15;
+    float top = kLowest;
+    for (uint32_t y = 0; y < nw; ++y) top = fmaxf(top, ml[2 * (y * nrows + m)]);
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (uint32_t y = 0; y < nw; ++y) {
+      const float ly = ml[2 * (y * nrows + m) + 1];
+      if (ly == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[2 * (y * nrows + m)] - top);
+      l = fmaf(ly, f, l);
+      const f32x4 oy = *reinterpret_cast<const f32x4*>(part + (y * nrows + m) * kD + 4 * (x ^ (m & 15)));
+      acc += oy * f;
+    }
+    if (p.splits > 1) {
+      const int64_t at = (int64_t)it * QB + m;
+      *reinterpret_cast<f32x4*>(p.part + at * kD + 4 * x) = acc;
+      if (x == 0) *reinterpret_cast<f32x2*>(p.part_ml + at * 2) = f32x2{top, l};
+    } else {
+      const Joined j = finish(top, l, p.off_by_one);
+      const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
+      store4(out0 + m * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
+      if (p.lse && x == 0)
+        p.lse[row0 + m0 + m] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+    }
+  }
+}
+
+// Joins the parts of split row blocks: 16 threads per row.
+template <typename T, int QB>
+__global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
+  const uint32_t e = __builtin_amdgcn_workgroup_id_x() * 256 + __builtin_amdgcn_workitem_id_x();
+  const uint32_t x = e & 15, m = (e >> 4) % QB, bb = (e >> 4) / QB;
+  const uint32_t bh = bb / p.blocks, blk = bb - bh * p.blocks;
+  if (bb >= p.items / p.splits) return;
+  uint32_t at0, nrows;
+  if (p.per_head) {
+    const uint32_t gh = blk / p.per_head, tmin = (blk - gh * p.per_head) * QB;
+    nrows = min((uint32_t)QB, p.T - tmin);
+    at0 = gh * p.T + tmin;
+  } else {
+    at0 = blk * QB;
+    nrows = min((uint32_t)QB, p.M - at0);
+  }
+  if (m >= nrows) return;
+  float top = kLowest;
+  for (uint32_t s = 0; s < p.splits; ++s)
+    top = fmaxf(top, p.part_ml[(((int64_t)bb * p.splits + s) * QB + m) * 2]);
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (uint32_t s = 0; s < p.splits; ++s) {
+    const int64_t at = ((int64_t)bb * p.splits + s) * QB + m;
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + at * 2);
+    if (ml[1] == 0.f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml[0] - top);
+    l = fmaf(ml[1], f, l);
+    acc += *reinterpret_cast<const f32x4*>(p.part + at * kD + 4 * x) * f;
+  }
+  const Joined j = finish(top, l, p.off_by_one);
+  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
+  const uint32_t b = bh / p.Hkv, h = bh - b * p.Hkv;
+  const int64_t r = (int64_t)(b * p.H + h * p.G) * p.T + at0 + m;
+  store4(reinterpret_cast<T*>(p.out) + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
+  if (p.lse && x == 0) p.lse[r] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+}
+
+}  // namespace
+
+namespace {
+constexpr int kWavesPerCu = 8;
+int most_waves(int rows) { return rows == 64 ? 4 : kMaxWaves; }  // (64 KiB of LDS for the parts)
+int rows_of(const gca_window& w, int64_t T) {
+  const int64_t M = w.H / w.Hkv * T;
+  return M <= 16 ? 16 : M <= 32 || w.dtype != GCA_BF16 ? 32 : 64;
+}
+// Tiles that a row block may see.
+int64_t tiles_seen(const gca_window& w, int64_t T, int rows) {
+  const int64_t all = w.capacity / 64, some = tiles_of(w.window + (T < rows ? T : rows) - 1);
+  return w.window && some < all ? some : all;
+}
+}  // namespace
+
+WindowAttnPlan window_attn_plan(const gca_window& w, int64_t T) {
+  WindowAttnPlan a;
+  const int64_t G = w.H / w.Hkv, M = G * T;
+  a.rows = rows_of(w, T);
+  a.per_head = T >= a.rows ? (T + a.rows - 1) / a.rows : 0;
+  a.blocks = a.per_head ? G * a.per_head : (M + a.rows - 1) / a.rows;
+  a.groups = (int64_t)w.B * w.Hkv * a.blocks;
+  const int64_t tiles = tiles_seen(w, T, a.rows), most = most_waves(a.rows), fill = kWavesPerCu * device_cus();
+  a.waves = 1;
+  while (a.waves < most && 2 * a.waves <= tiles && a.groups * a.waves < fill) a.waves *= 2;
+  // more workgroups where that leaves each wave two tiles at least
+  int64_t splits = 1;
+  if (a.waves == most) {
+    splits = fill / (a.groups * most);
+    if (splits > tiles / (2 * most)) splits = tiles / (2 * most);
+  }
+  a.splits = (int)(splits < 1 ? 1 : splits);
+  return a;
+}
+
+size_t window_workspace(const gca_window& w, int64_t T) {
+  // (what any number of row blocks of this height asks for: it then never falls as T grows)
+  const int rows = rows_of(w, T), most = most_waves(rows);
+  if (tiles_seen(w, T, rows) < 4 * most) return 0;
+  return align256((size_t)(kWavesPerCu * device_cus() / most) * rows * (kD + 2) * sizeof(float));
+}
+
+hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t* parents, const int32_t* lengths,
+                              const float* slopes, void* out, float* lse, int64_t T, void* ws, hipStream_t stream) {
+  const WindowAttnPlan a = window_attn_plan(w, T);
+  WindowParams p;
+  p.items = (uint32_t)(a.groups * a.splits);
+  p.splits = (uint32_t)a.splits;
+  p.blocks = (uint32_t)a.blocks;
+  p.nw = (uint32_t)a.waves;
+  p.Hkv = w.Hkv;
+  p.H = w.H;
+  p.G = w.H / w.Hkv;
+  p.T = (uint32_t)T;
+  p.M = (uint32_t)(p.G * T);
+  p.per_head = (uint32_t)a.per_head;
+  p.ring_tiles = (uint32_t)(w.capacity / 64);
+  p.ring = w.window > 0;
+  p.window = w.window;
+  p.length = w.length;
+  p.parents = parents;
+  p.lengths = lengths;
+  p.slopes = slopes;
+  p.k = static_cast<const uint8_t*>(w.k);
+  p.v = static_cast<const uint8_t*>(w.v);
+  p.ks = w.k_scale;
+  p.vs = w.v_scale;
+  p.q = q;
+  p.out = out;
+  p.lse = lse;
+  p.part = static_cast<float*>(ws);
+  p.part_ml = p.part + (size_t)a.groups * a.splits * a.rows * kD;
+  const float s = fabsf(w.attn_scale);
+  p.scale = (s > 0.f ? s : 1.f) * kLog2e;
+  p.unscale = s > 0.f ? 1.f / s : 1.f;
+  p.negate = w.attn_scale < 0.f ? (w.dtype == GCA_BF16 ? 0x80008000u : 0x80000000u) : 0u;
+  p.keep = s > 0.f ? 0xffffffffu : 0u;
+  p.off_by_one = w.off_by_one;
+  size_t lds = (size_t)a.waves * 128 * sizeof(float);
+  const size_t parts = a.waves * a.splits > 1 ? (size_t)a.waves * a.rows * (kD + 2) * sizeof(float) : 0;
+  if (parts > lds) lds = parts;
+  const dim3 grid((p.items + 7) / 8 * 8), block(64 * a.waves);
+  auto run = [&](auto tag, auto i8) {
+    using T_ = decltype(tag);
+    constexpr bool I8 = decltype(i8)::value;
+    const char* name = "window_attn_kernel";
+    if (a.rows == 16) launch_kernel(name, window_attn_kernel<T_, I8, 16, 1>, grid, block, lds, stream, p);
+    else if (a.rows == 32) launch_kernel(name, window_attn_kernel<T_, I8, 32, 1>, grid, block, lds, stream, p);
+    else if constexpr (sizeof(T_) == 2)
+      launch_kernel(name, window_attn_kernel<T_, I8, 32, 2>, grid, block, lds, stream, p);
+    if (a.splits > 1) {
+      const dim3 joins((unsigned)((a.groups * a.rows * 16 + 255) / 256)), threads(256);
+      name = "window_join_kernel";
+      if (a.rows == 16) launch_kernel(name, window_join_kernel<T_, 16>, joins, threads, 0, stream, p);
+      else if (a.rows == 32) launch_kernel(name, window_join_kernel<T_, 32>, joins, threads, 0, stream, p);
+      else if constexpr (sizeof(T_) == 2) launch_kernel(name, window_join_kernel<T_, 64>, joins, threads, 0, stream, p);
+    }
+  };
+  if (w.dtype == GCA_BF16) w.format == GCA_INT8 ? run(__bf16{}, std::true_type{}) : run(__bf16{}, std::false_type{});
+  else w.format == GCA_INT8 ? run(float{}, std::true_type{}) : run(float{}, std::false_type{});
+  return take_launch_error();
+}
+
+}  // namespace gca

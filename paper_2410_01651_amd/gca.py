@@ -26,6 +26,12 @@ EXPORTS = (
     "gca_cache_xattn",
     "gca_cache_evict",
     "gca_cache_workspace_size",
+    "gca_window_append",
+    "gca_window_attn",
+    "gca_window_keep",
+    "gca_window_workspace_size",
+    "gca_verify",
+    "gca_verify_workspace_size",
     "gca_workspace_size",
     "gca_status_string",
     "gca_last_error",
@@ -106,6 +112,30 @@ class CacheStruct(ctypes.Structure):
     ]
 
 
+class WindowStruct(ctypes.Structure):
+    """Mirror of ``gca_window``."""
+
+    _fields_ = [
+        ("B", ctypes.c_int32),
+        ("H", ctypes.c_int32),
+        ("Hkv", ctypes.c_int32),
+        ("d", ctypes.c_int32),
+        ("capacity", ctypes.c_int64),
+        ("window", ctypes.c_int32),
+        ("attn_scale", ctypes.c_float),
+        ("off_by_one", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("length", ctypes.c_void_p),
+        ("ticket", ctypes.c_void_p),
+    ]
+
+
 class GcaError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(message)
@@ -124,7 +154,7 @@ def lib():
                                "`python -m paper_2410_01651_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
         vp, P = ctypes.c_void_p, ctypes.POINTER(Problem)
-        C, i64 = ctypes.POINTER(CacheStruct), ctypes.c_int64
+        C, W, i64 = ctypes.POINTER(CacheStruct), ctypes.POINTER(WindowStruct), ctypes.c_int64
         sig = {
             "gca_chunk_scores": [P, vp, vp, vp, vp],
             "gca_topk": [P, vp, vp, vp, vp],
@@ -138,6 +168,10 @@ def lib():
             "gca_cache_xattn": [C, vp, vp, vp, vp, vp, vp, i64, i64, ctypes.c_int32, vp],
             "gca_cache_evict": [C, vp, vp, i64, ctypes.c_float, ctypes.c_int32, ctypes.c_int32, vp, vp, i64, vp,
                                 ctypes.c_size_t, vp],
+            "gca_window_append": [W, vp, vp, vp, i64, vp],
+            "gca_window_attn": [W, vp, vp, vp, vp, vp, vp, i64, vp, ctypes.c_size_t, vp],
+            "gca_window_keep": [W, vp, i64, vp, i64, vp],
+            "gca_verify": [i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -145,6 +179,10 @@ def lib():
             fn.restype = ctypes.c_int
         L.gca_cache_workspace_size.argtypes = [C, ctypes.c_int, i64]
         L.gca_cache_workspace_size.restype = ctypes.c_size_t
+        L.gca_window_workspace_size.argtypes = [W, i64]
+        L.gca_window_workspace_size.restype = ctypes.c_size_t
+        L.gca_verify_workspace_size.argtypes = [i64, i64, i64]
+        L.gca_verify_workspace_size.restype = ctypes.c_size_t
         L.gca_workspace_size.argtypes = [P, ctypes.c_int]
         L.gca_workspace_size.restype = ctypes.c_size_t
         L.gca_status_string.argtypes = [ctypes.c_int]
@@ -450,6 +488,27 @@ def cache_shapes(B, Hkv, capacity, Hr, D):
                 number=(B, capacity), next=(B,))
 
 
+def _members(shapes, types, tensors, device, what):
+    """A handle's tensors by name, those not given allocated as zeros, and their device."""
+    torch = _torch()
+    given = dict(tensors or {})
+    if not set(given) <= set(shapes):
+        raise ValueError(f"a {what} has no tensors named {sorted(set(given) - set(shapes))}")
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"a {what} lives in device memory")
+    if device.index is None:
+        device = next(iter(given.values())).device if given else torch.device("cuda", torch.cuda.current_device())
+    for name, t in given.items():
+        _ptr(t, name, types[name], shapes[name])
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the {what} on {device}")
+    for name in shapes:
+        if name not in given:
+            given[name] = torch.zeros(shapes[name], dtype=types[name], device=device)
+    return given, device
+
+
 def cache(B, H, capacity, topk, Hkv=None, Hr=1, D=None, score_scale=None, attn_scale=None, off_by_one=False,
           dtype="bf16", format="e4m3", device="cuda", tensors=None) -> Cache:
     """A cache of `capacity` chunks for each of B sequences, all slots free.  Hkv defaults to H, D
@@ -462,21 +521,7 @@ def cache(B, H, capacity, topk, Hkv=None, Hr=1, D=None, score_scale=None, attn_s
     types = dict(k=num, v=num, k_scale=torch.float32, v_scale=torch.float32, lmk=elem, tokens=torch.int32,
                  mass=torch.float32, number=torch.int32, next=torch.int32)
     sh = cache_shapes(B, Hkv, capacity, Hr, D)
-    given = dict(tensors or {})
-    if not set(given) <= set(sh):
-        raise ValueError(f"a cache has no tensors named {sorted(set(given) - set(sh))}")
-    device = torch.device(device)
-    if device.type != "cuda":
-        raise ValueError("a cache lives in device memory")
-    if device.index is None:
-        device = next(iter(given.values())).device if given else torch.device("cuda", torch.cuda.current_device())
-    for name, t in given.items():
-        _ptr(t, name, types[name], sh[name])
-        if t.device != device:
-            raise ValueError(f"{name} is on {t.device}, the cache on {device}")
-    for name in sh:
-        if name not in given:
-            given[name] = torch.zeros(sh[name], dtype=types[name], device=device)
+    given, device = _members(sh, types, tensors, device, "cache")
     struct = CacheStruct(
         B=B, H=H, Hkv=Hkv, Hr=Hr, d=64, S=64, capacity=capacity, topk=topk, D=D,
         score_scale=1.0 / math.sqrt(D) if score_scale is None else score_scale,
@@ -536,7 +581,7 @@ def _at(c: Cache, stream):
             return c.here
         return _There(torch.cuda.device(c.index), c)
     if stream.device != c.device:
-        raise ValueError(f"the stream is on {stream.device}, the cache on {c.device}")
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {c.device}")
     return _There(torch.cuda.stream(stream), c)
 
 
@@ -548,7 +593,7 @@ def _cache_ptr(c: Cache, t, name, dtype, shape):
     if t.get_device() == c.index and t.dtype is dtype and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
     if t.device != c.device:
-        raise ValueError(f"{name} must be on the cache's device {c.device}, got {t.device}")
+        raise ValueError(f"{name} must be on device {c.device}, got {t.device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
@@ -650,6 +695,186 @@ def cache_evict(c: Cache, n, idx=None, w=None, decay=1.0, keep_first=0, keep_las
         _check(lib().gca_cache_evict(c.ref, ip, wp, nQ, decay, keep_first, keep_last, want_p, sp if n else None, n,
                                      _cache_ptr(c, ws, "workspace", c.torch.uint8, ws.shape), ws.numel(), st))
     return slots
+
+
+# ------------------------------------------------------------- token window ----
+
+class Window:
+    """The tokens that a layer's self-attention looks back at, in 8 bits (``gca_window``): its sizes and
+    its device tensors, which are the program's own and may be read or, between calls, changed in place:
+
+    * ``k`` [B, Hkv, C, 64], ``v`` [B, Hkv, C / 64, 64, 64 tokens]: 8-bit numbers
+      (``torch.float8_e4m3fn`` or ``torch.int8``), values transposed per 64 rows;
+    * ``k_scale``, ``v_scale`` [B, Hkv, C] fp32: a number stands for itself times its token's;
+    * ``length`` [B] int32: tokens of each sequence so far (position p is in row p mod C, or with
+      window = 0 in row p); ``ticket`` [B, 2 H] int32: zeros between calls.
+
+    To give sequence b's place to another sequence, zero ``length[b]``."""
+
+    NAMES = ("k", "v", "k_scale", "v_scale", "length", "ticket")
+
+    def __init__(self, struct, tensors, device, index):
+        self.torch = torch = _torch()
+        self.struct = struct
+        self.ref = ctypes.byref(struct)
+        self.device = device
+        self.index = index    # the device's ordinal
+        self.here = _Here(torch, index)
+        self.dims = struct.B, struct.H, struct.Hkv
+        self.elem = torch.bfloat16 if struct.dtype == GCA_BF16 else torch.float32
+        for name in self.NAMES:
+            setattr(self, name, tensors[name])
+
+
+def window_shapes(B, H, Hkv, capacity):
+    """Shapes of a window's tensors, by name."""
+    return dict(k=(B, Hkv, capacity, 64), v=(B, Hkv, capacity // 64, 64, 64), k_scale=(B, Hkv, capacity),
+                v_scale=(B, Hkv, capacity), length=(B,), ticket=(B, 2 * H))
+
+
+def window(B, H, capacity, window=0, Hkv=None, attn_scale=None, off_by_one=False, dtype="bf16", format="e4m3",
+           device="cuda", tensors=None) -> Window:
+    """A window of `capacity` rows (a multiple of 64) for each of B sequences, empty.  A row sees `window`
+    tokens, itself included (0: all).  Hkv defaults to H, the scale to 1/sqrt(64); ``format`` is
+    "e4m3" or "int8".  Members named in ``tensors`` are taken as they are instead of allocated."""
+    torch = _torch()
+    Hkv = H if Hkv is None else Hkv
+    num = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}[format]
+    types = dict(k=num, v=num, k_scale=torch.float32, v_scale=torch.float32, length=torch.int32, ticket=torch.int32)
+    struct = WindowStruct(
+        B=B, H=H, Hkv=Hkv, d=64, capacity=capacity, window=window, attn_scale=0.125 if attn_scale is None else attn_scale,
+        off_by_one=int(bool(off_by_one)), dtype={"bf16": GCA_BF16, "fp32": GCA_FP32}[dtype],
+        format=GCA_E4M3 if format == "e4m3" else GCA_INT8, flags=0)
+    sh = window_shapes(B, H, Hkv, capacity)
+    given, device = _members(sh, types, tensors, device, "window")
+    for name in sh:
+        setattr(struct, name, given[name].data_ptr())
+    return Window(struct, given, device, device.index)
+
+
+def window_workspace_size(w: Window, T: int) -> int:
+    return int(lib().gca_window_workspace_size(w.ref, T))
+
+
+def window_workspace(w: Window, T: int):
+    """Workspace of window_attn of up to T tokens, on the window's device."""
+    size = window_workspace_size(w, T)
+    return _torch().empty(max(size, 1), dtype=_torch().uint8, device=w.device), size
+
+
+def window_append(w: Window, k, v, lengths=None, stream=None):
+    """gca_window_append: T new tokens' keys and values k, v [B, Hkv, T, 64]; lengths [B]: how many of them
+    each sequence has."""
+    B, _, Hkv = w.dims
+    if k.dim() != 4:
+        raise ValueError("k must have shape (B, Hkv, T, 64)")
+    T = k.shape[2]
+    kv = (B, Hkv, T, 64)
+    with _at(w, stream) as st:
+        _check(lib().gca_window_append(w.ref, _cache_ptr(w, k, "k", w.elem, kv), _cache_ptr(w, v, "v", w.elem, kv),
+                                       _cache_ptr(w, lengths, "lengths", w.torch.int32, (B,)), T, st))
+
+
+def window_attn(w: Window, q, parents=None, lengths=None, slopes=None, out=None, lse=None, want_lse=True, ws=None,
+                stream=None):
+    """gca_window_attn: the newest T tokens' queries q [B, H, T, 64] against the window; parents [B, T]: their
+    tree (a chain without), lengths [B]: how many of them each sequence has, slopes [H]: linear biases.
+    Returns out, lse [B, H, T]."""
+    i32, f32 = w.torch.int32, w.torch.float32
+    B, H, _ = w.dims
+    if q.dim() != 4:
+        raise ValueError("q must have shape (B, H, T, 64)")
+    T = q.shape[2]
+    qs = (B, H, T, 64)
+    qp, op = _cache_ptr(w, q, "q", w.elem, qs), _cache_ptr(w, out, "out", w.elem, qs)
+    pp, np_ = _cache_ptr(w, parents, "parents", i32, (B, T)), _cache_ptr(w, lengths, "lengths", i32, (B,))
+    sp, lp = _cache_ptr(w, slopes, "slopes", f32, (H,)), _cache_ptr(w, lse, "lse", f32, (B, H, T))
+    with _at(w, stream) as st:
+        if out is None:
+            out, op = _new(w, qs, w.elem, q)
+        if lse is None and want_lse:
+            lse, lp = _new(w, (B, H, T), f32)
+        if ws is None:
+            ws = window_workspace(w, T)[0]
+        _check(lib().gca_window_attn(w.ref, qp, pp, np_, sp, op, lp, T,
+                                     _cache_ptr(w, ws, "workspace", w.torch.uint8, ws.shape), ws.numel(), st))
+    return out, lse
+
+
+def window_keep(w: Window, T, path, lengths=None, stream=None):
+    """gca_window_keep: of the newest T tokens (lengths [B] of each sequence's) keep those that path [B, n]
+    names, and drop the others."""
+    i32 = w.torch.int32
+    B = w.dims[0]
+    if path.dim() != 2:
+        raise ValueError("path must have shape (B, n)")
+    n = path.shape[1]
+    with _at(w, stream) as st:
+        _check(lib().gca_window_keep(w.ref, _cache_ptr(w, path, "path", i32, (B, n)), n,
+                                     _cache_ptr(w, lengths, "lengths", i32, (B,)), T, st))
+
+
+# ------------------------------------------------------ verification of drafts ----
+
+class _Place:
+    """The device of a call without a handle, as the checks above ask for it."""
+
+    def __init__(self, device):
+        self.torch = _torch()
+        self.device, self.index = device, device.index
+        self.here = _Here(self.torch, device.index)
+
+
+_places = {}
+
+
+def _place(t, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    i = t.get_device()
+    if i not in _places:
+        _places[i] = _Place(t.device)
+    return _places[i]
+
+
+def verify_workspace_size(B: int, T: int, V: int) -> int:
+    return int(lib().gca_verify_workspace_size(B, T, V))
+
+
+def verify_workspace(B: int, T: int, V: int, device="cuda"):
+    size = verify_workspace_size(B, T, V)
+    return _torch().empty(max(size, 1), dtype=_torch().uint8, device=device), size
+
+
+def verify(p, tokens, u, q=None, parents=None, lengths=None, path=None, count=None, next=None, ws=None, stream=None):
+    """gca_verify: drafted tokens [B, T] (node 0: the newest token itself) of a tree (parents [B, T]; a
+    chain without) against the target's probabilities p [B, T, V], with random numbers u [B, T]; q [B, T, V]:
+    the probabilities that the drafts were drawn from (None: they were chosen); lengths [B]: nodes of each
+    sequence.  Returns path [B, T], count [B], next [B]."""
+    c = _place(p, "p")
+    i32, f32 = c.torch.int32, c.torch.float32
+    if p.dim() != 3:
+        raise ValueError("p must have shape (B, T, V)")
+    B, T, V = p.shape
+    bt = (B, T)
+    qp = _cache_ptr(c, q, "q", f32, p.shape)
+    tp, up = _cache_ptr(c, tokens, "tokens", i32, bt), _cache_ptr(c, u, "u", f32, bt)
+    rp, np_ = _cache_ptr(c, parents, "parents", i32, bt), _cache_ptr(c, lengths, "lengths", i32, (B,))
+    pp = _cache_ptr(c, p, "p", f32, p.shape)
+    op, cp = _cache_ptr(c, path, "path", i32, bt), _cache_ptr(c, count, "count", i32, (B,))
+    xp = _cache_ptr(c, next, "next", i32, (B,))
+    with _at(c, stream) as st:
+        if path is None:
+            path, op = _new(c, bt, i32, tokens)
+        if count is None:
+            count, cp = _new(c, (B,), i32)
+        if next is None:
+            next, xp = _new(c, (B,), i32)
+        if ws is None:
+            ws = verify_workspace(B, T, V, c.device)[0]
+        _check(lib().gca_verify(B, T, V, pp, qp, tp, rp, up, np_, op, cp, xp,
+                                _cache_ptr(c, ws, "workspace", c.torch.uint8, ws.shape), ws.numel(), st))
+    return path, count, next
 
 
 # ---------------------------------------------------------------- profiling ----
