@@ -443,7 +443,7 @@ gca_status gca_window_attn(const gca_window* w, const void* q, const int32_t* pa
  * outside 0 .. n_b - 1 (-1 padding).
  *   path    [B, n] int32, 0 <= n <= 64 (e.g. from gca_verify)
  *   lengths [B]    int32, as for the append; may be NULL
- * Requires w->k, v, k_scale, v_scale, length.  T >= 1; in a ring T <= capacity. */
+ * Requires w->k, v, k_scale, v_scale, length, ticket.  T >= 1; in a ring T <= capacity. */
 gca_status gca_window_keep(const gca_window* w, const int32_t* path, int64_t n, const int32_t* lengths, int64_t T,
                            hipStream_t stream);
 

@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kVerifyThreads = 256;
 constexpr int kVerifyWaves = kVerifyThreads / 64;
+constexpr int kPerThread = 8;  // consecutive entries of a thread where order counts
 constexpr double kFix = 17592186044416.0;       // 2^44
 constexpr double kUnfix = 1.0 / 17592186044416.0;
 
@@ -47,9 +48,9 @@ struct VerifyParams {
   int32_t* count;
   int32_t* next;
   Walk* walk;      // [B]
-  int64_t* sums;   // [B][slices]
+  int64_t* sums;   // [B][slices][waves]
   uint32_t B, T, slices;
-  uint32_t V, per;  // entries in all, and per slice (a multiple of 4)
+  uint32_t V, per;  // entries in all, and per wave of a slice (a multiple of 4)
 };
 
 // A probability as it counts.
@@ -63,11 +64,27 @@ __device__ __forceinline__ double less(double r, double z, double q) {
   const double d = r - s;
   return d > 0.0 ? d : 0.0;
 }
+// Whether u z q < r: two products, each rounded.
+__device__ __forceinline__ bool test(double u, double z, double q, double r) {
+#pragma clang fp contract(off)
+  const double s = z * q;
+  const double us = u * s;
+  return us < r;
+}
 // r in whole multiples of 2^-44, to the nearest (ties to even): 0 .. 2^44, so the sum with 2^52 holds it
 // in its mantissa.
 __device__ __forceinline__ int64_t whole(double r) {
   const double x = r * kFix + 4503599627370496.0;
   return __double_as_longlong(x) & 0xfffffffffffffll;
+}
+
+// Lane c's value, c the same in every lane.
+__device__ __forceinline__ int lane_of(int x, int c) { return __builtin_amdgcn_readlane(x, c); }
+__device__ __forceinline__ double lane_of(double x, int c) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, c);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), c);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 
 __device__ __forceinline__ int64_t wave_sum(int64_t x) {
@@ -76,37 +93,71 @@ __device__ __forceinline__ int64_t wave_sum(int64_t x) {
   return x;
 }
 
-// r[x] of the walk's last node.
-__device__ __forceinline__ double left(const Walk& w, bool drawn, float p, float q, uint32_t x) {
-  double r = prob(p);
-  if (drawn) {
-    const double c = prob(q);
-    for (int j = 0; j < w.rejected; ++j) r = less(r, w.z[j], c);
-  } else {
-    for (int j = 0; j < w.rejected; ++j)
-      if (w.token[j] == (int32_t)x) r = 0.0;
-  }
-  return r;
-}
-
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4u;
 
-// This thread's part of the sum of r over entries [lo, hi) of the last node's row; `plain`: of p[a] itself.
+// What the rejections at the walk's last node leave of N consecutive entries from x on, as whole numbers;
+// `chosen`: of the rejected tokens too.
+template <int N>
+__device__ __forceinline__ void left(const Walk& w, bool drawn, bool chosen, const float* p, const float* q, uint32_t x,
+                                     int64_t* out) {
+  double r[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) r[e] = prob(p[e]);
+  if (drawn)
+    for (int j = 0; j < w.rejected; ++j) {
+      const double z = w.z[j];
+#pragma unroll
+      for (int e = 0; e < N; ++e) r[e] = less(r[e], z, prob(q[e]));
+    }
+  else if (chosen)
+    for (int j = 0; j < w.rejected; ++j) {
+      const uint32_t t = (uint32_t)w.token[j];
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (t == x + e) r[e] = 0.0;
+    }
+#pragma unroll
+  for (int e = 0; e < N; ++e) out[e] = whole(r[e]);
+}
+
+// Part `part` of `parts` (lanes or threads) of the sum of r over entries [lo, hi) of the last node's row, four
+// consecutive entries at a time; `plain`: of p[a] itself.
 __device__ __forceinline__ int64_t part_sum(const VerifyParams& p, const Walk& w, uint32_t b, uint32_t lo, uint32_t hi,
-                                            bool plain) {
+                                            bool plain, uint32_t part, uint32_t parts) {
   const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
   const float* pr = p.p + row;
-  const bool drawn = p.q != nullptr, with_q = drawn && w.rejected > 0 && !plain;
-  const float* qr = with_q ? p.q + row : pr;
+  const bool drawn = p.q != nullptr && w.rejected > 0 && !plain;
   int64_t sum = 0;
-  for (uint32_t x = lo + 4 * threadIdx.x; x < hi; x += 4 * kVerifyThreads) {
-    if (x + 4 <= hi) {
+  uint32_t x = lo + 4 * part;
+  if (drawn) {
+    const float* qr = p.q + row;
+#pragma unroll 4
+    for (; x + 4 <= hi; x += 4 * parts) {
       const f32x4u a = *reinterpret_cast<const f32x4u*>(pr + x), c = *reinterpret_cast<const f32x4u*>(qr + x);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += whole(plain ? prob(a[e]) : left(w, drawn, a[e], c[e], x + e));
-    } else {
-      for (uint32_t y = x; y < hi; ++y) sum += whole(plain ? prob(pr[y]) : left(w, drawn, pr[y], qr[y], y));
+      const float pe[4] = {a[0], a[1], a[2], a[3]}, qe[4] = {c[0], c[1], c[2], c[3]};
+      int64_t r[4];
+      left<4>(w, true, false, pe, qe, x, r);
+      sum += r[0] + r[1] + r[2] + r[3];
     }
+    for (; x < hi; ++x) {
+      int64_t r;
+      left<1>(w, true, false, pr + x, qr + x, x, &r);
+      sum += r;
+    }
+    return sum;
+  }
+#pragma unroll 8
+  for (; x + 4 <= hi; x += 4 * parts) {
+    const f32x4u a = *reinterpret_cast<const f32x4u*>(pr + x);
+    sum += whole(prob(a[0])) + whole(prob(a[1])) + whole(prob(a[2])) + whole(prob(a[3]));
+  }
+  for (; x < hi; ++x) sum += whole(prob(pr[x]));
+  // (chosen tokens that were rejected: taken off again, each once)
+  if (!plain && p.q == nullptr && part < (uint32_t)w.rejected) {
+    const uint32_t t = (uint32_t)w.token[part];
+    bool once = t >= lo && t < hi;
+    for (uint32_t j = 0; j < part; ++j) once = once && (uint32_t)w.token[j] != t;
+    if (once) sum -= whole(prob(pr[t]));
   }
   return sum;
 }
@@ -155,25 +206,46 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
   int cur = n > 0 ? 0 : -1, rejected = 0;
   uint64_t on = n > 0 ? 1 : 0, done = 0;  // accepted nodes; tested ones
   double z = 1.0;
+  // Every node's test at once, as it comes out if the siblings before it are rejected.  Where drafts are drawn
+  // that holds for first children; where they are chosen a node's z is what they leave.
+  const uint64_t valid = __ballot(real);
+  uint64_t accept = 0;
+  if (first_wave) {
+    double mine = 1.0;
+    if (!drawn)
+      for (uint64_t c = valid; c != 0; c &= c - 1) {
+        const int i = __builtin_ctzll(c);
+        const bool later = real && lane > i && par == lane_of(par, i);
+        if (__ballot(later) == 0) continue;
+        const double d = mine - lane_of(r, i);
+        if (later) {
+          mine = d > 0.0 ? d : 0.0;
+          if (tok == lane_of(tok, i)) r = 0.0;
+        }
+      }
+    accept = __ballot(real && test((double)u, mine, q, r));
+  }
   for (;;) {
     if (first_wave) {
       again = 0;
       for (;;) {
-        const uint64_t open = cur < 0 ? 0 : __ballot(lane < n && par == cur) & ~done;
+        const uint64_t open = cur < 0 ? 0 : __ballot(par == cur) & valid & ~done;
         if (open == 0) break;
+        if (!drawn) {
+          const uint64_t taken = open & accept;
+          if (taken == 0) {
+            rejected = __builtin_popcountll(open);
+            if (open >> lane & 1) w.token[lanes_below(open)] = tok;
+            break;
+          }
+          cur = __builtin_ctzll(taken);
+          on |= 1ull << cur;
+          continue;
+        }
         const int c = __builtin_ctzll(open);
         done |= 1ull << c;
-        const double rc = __shfl(r, c), qc = __shfl(q, c);
-        const double uc = (double)__shfl(u, c);
-        const int tc = __shfl(tok, c);
-        if (!__shfl((int)real, c)) continue;
-        bool take;
-        {
-#pragma clang fp contract(off)
-          const double s = z * qc;
-          const double us = uc * s;
-          take = us < rc;
-        }
+        const bool take = rejected == 0 ? accept >> c & 1
+                                        : test(lane_of((double)u, c), z, lane_of(q, c), lane_of(r, c));
         if (take) {
           cur = c;
           on |= 1ull << c;
@@ -181,20 +253,12 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
           z = 1.0;
           continue;
         }
-        if (drawn) {
-          if (lane == 0) w.z[rejected] = z;
-          ++rejected;
-          if (par == cur) r = less(r, z, q);
-          if ((open & (open - 1)) != 0) {  // a sibling is left: its test needs the sum
-            again = 1;
-            break;
-          }
-        } else {
-          if (lane == 0) w.token[rejected] = tc;
-          ++rejected;
-          const double d = z - rc;
-          z = d > 0.0 ? d : 0.0;
-          if (par == cur && tok == tc) r = 0.0;
+        if (lane == 0) w.z[rejected] = z;
+        ++rejected;
+        if (par == cur) r = less(r, z, q);
+        if ((open & (open - 1)) != 0) {  // a sibling is left: its test needs the sum
+          again = 1;
+          break;
         }
       }
       if (lane == 0) {
@@ -205,7 +269,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
     }
     __syncthreads();
     if (!again) break;
-    const int64_t s = block_sum(part_sum(p, w, b, 0, p.V, false), lds);
+    const int64_t s = block_sum(part_sum(p, w, b, 0, p.V, false, threadIdx.x, kVerifyThreads), lds);
     z = (double)s * kUnfix;
     __syncthreads();  // (`again` and the walk are read before they are written again)
   }
@@ -223,9 +287,11 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
       reinterpret_cast<uint32_t*>(p.walk + b)[x] = reinterpret_cast<const uint32_t*>(&w)[x];
   }
   if (w.node < 0) return;
-  const uint32_t lo = slice * p.per, hi = min(lo + p.per, p.V);
-  const int64_t s = block_sum(part_sum(p, w, b, lo, hi, false), lds);
-  if (threadIdx.x == 0) p.sums[(int64_t)b * p.slices + slice] = s;
+  // one sum per wave, each of a quarter of the slice
+  const uint32_t quarter = slice * kVerifyWaves + (threadIdx.x >> 6);
+  const uint32_t lo = min(quarter * p.per, p.V), hi = min(lo + p.per, p.V);
+  const int64_t s = wave_sum(part_sum(p, w, b, lo, hi, false, lane, 64));
+  if (lane == 0) p.sums[(int64_t)b * p.slices * kVerifyWaves + quarter] = s;
 }
 
 // One workgroup per sequence: the slice that the drawn place is in, and the token in it.
@@ -246,14 +312,32 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParam
     return;
   }
   const bool drawn = p.q != nullptr;
-  // (one slice per thread: at most kVerifyThreads of them)
-  int64_t mine = tid < (int)p.slices ? p.sums[(int64_t)b * p.slices + tid] : 0;
+  // (four sums per thread, its slice's)
+  int64_t part[kVerifyWaves], mine = 0;
+#pragma unroll
+  for (int e = 0; e < kVerifyWaves; ++e) {
+    part[e] = tid < (int)p.slices ? p.sums[((int64_t)b * p.slices + tid) * kVerifyWaves + e] : 0;
+    mine += part[e];
+  }
   bool plain = false;
-  int64_t total = block_sum(mine, lds);
+  int64_t upto = mine;  // sum of the slices up to this one
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const int64_t y = __shfl_up(upto, s);
+    if (lane >= s) upto += y;
+  }
+  if (lane == 63) lds[tid >> 6] = upto;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int y = 0; y < kVerifyWaves; ++y) {
+    if (y < (tid >> 6)) upto += lds[y];
+    total += lds[y];
+  }
   uint32_t lo = 0, hi = p.V;
   if (total == 0) {  // nothing is left: of p itself, the whole vocabulary as one slice
     plain = true;
-    total = block_sum(part_sum(p, w, b, 0, p.V, true), lds);
+    total = block_sum(part_sum(p, w, b, 0, p.V, true, threadIdx.x, kVerifyThreads), lds);
     if (total == 0) {
       if (tid == 0) p.next[b] = -1;
       return;
@@ -261,34 +345,58 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParam
     if (tid == 0) place = (int64_t)((double)u * (double)total);
     __syncthreads();
   } else {
-    const int64_t at = (int64_t)((double)u * (double)total);
-    int64_t upto = mine;  // sum of the slices up to this one
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      const int64_t y = __shfl_up(upto, s);
-      if (lane >= s) upto += y;
-    }
-    __syncthreads();
-    if (lane == 63) lds[tid >> 6] = upto;
-    __syncthreads();
-    for (int y = 0; y < (tid >> 6); ++y) upto += lds[y];
+    int64_t at = (int64_t)((double)u * (double)total);
     if (upto > at && upto - mine <= at) {  // one thread
-      chosen = tid;
-      place = at - (upto - mine);
+      at -= upto - mine;
+      uint32_t e = 0;
+#pragma unroll
+      for (int y = 0; y < kVerifyWaves - 1; ++y)
+        if (e == (uint32_t)y && at >= part[y]) {
+          at -= part[y];
+          ++e;
+        }
+      chosen = tid * kVerifyWaves + e;
+      place = at;
     }
     __syncthreads();
     lo = chosen * p.per;
     hi = min(lo + p.per, p.V);
   }
-  // blocks of entries in order, one per thread and step
+  // blocks of entries in order, kPerThread consecutive ones per thread
   const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
   const float* pr = p.p + row;
   const float* qr = drawn && w.rejected > 0 ? p.q + row : pr;
   int64_t before = 0;
-  for (uint32_t x0 = lo; x0 < hi; x0 += kVerifyThreads) {
-    const uint32_t x = x0 + tid;
-    const int64_t r = x < hi ? whole(plain ? prob(pr[x]) : left(w, drawn, pr[x], qr[x], x)) : 0;
-    int64_t upto = r;
+  for (uint32_t x0 = lo; x0 < hi; x0 += kVerifyThreads * kPerThread) {
+    const uint32_t x = x0 + tid * kPerThread;
+    f32x4u a[kPerThread / 4], c[kPerThread / 4];
+    if (x + kPerThread <= p.V) {
+#pragma unroll
+      for (int e = 0; e < kPerThread / 4; ++e) {
+        a[e] = *reinterpret_cast<const f32x4u*>(pr + x + 4 * e);
+        c[e] = *reinterpret_cast<const f32x4u*>(qr + x + 4 * e);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kPerThread; ++e) {
+        a[e / 4][e % 4] = x + e < p.V ? pr[x + e] : 0.f;
+        c[e / 4][e % 4] = x + e < p.V ? qr[x + e] : 0.f;
+      }
+    }
+    float pe[kPerThread], qe[kPerThread];
+    int64_t r[kPerThread], mine = 0;
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) {
+      pe[e] = a[e / 4][e % 4];
+      qe[e] = c[e / 4][e % 4];
+    }
+    left<kPerThread>(w, drawn && !plain, !plain, pe, qe, x, r);
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) {
+      r[e] = x + e < hi ? r[e] : 0;
+      mine += r[e];
+    }
+    int64_t upto = mine;
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) {
       const int64_t y = __shfl_up(upto, s);
@@ -298,12 +406,22 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParam
     if (lane == 63) lds[tid >> 6] = upto;
     __syncthreads();
     int64_t step = 0;
+#pragma unroll
     for (int y = 0; y < kVerifyWaves; ++y) {
       if (y < (tid >> 6)) upto += lds[y];
       step += lds[y];
     }
     upto += before;
-    if (upto > place && upto - r <= place) p.next[b] = (int32_t)x;
+    if (upto > place && upto - mine <= place) {  // one thread
+      int64_t at = upto - mine;
+      uint32_t found = x;
+#pragma unroll
+      for (int e = 0; e < kPerThread; ++e) {
+        at += r[e];
+        if (at <= place) found = x + e + 1;
+      }
+      p.next[b] = (int32_t)found;
+    }
     before += step;
     if (before > place) break;  // (uniform)
   }
@@ -319,14 +437,14 @@ VerifyPlan verify_plan(int64_t B, int64_t V) {
   if (slices > kVerifyThreads) slices = kVerifyThreads;
   if (slices < 1) slices = 1;
   VerifyPlan a;
-  a.per = ((V + slices - 1) / slices + 3) / 4 * 4;
-  a.slices = (V + a.per - 1) / a.per;
+  a.per = ((V + slices * kVerifyWaves - 1) / (slices * kVerifyWaves) + 3) / 4 * 4;
+  a.slices = (V + a.per * kVerifyWaves - 1) / (a.per * kVerifyWaves);
   return a;
 }
 
 size_t verify_workspace(int64_t B, int64_t T, int64_t V) {
   (void)T;
-  return align256((size_t)B * sizeof(Walk)) + align256((size_t)B * verify_plan(B, V).slices * sizeof(int64_t));
+  return align256((size_t)B * sizeof(Walk)) + align256((size_t)B * verify_plan(B, V).slices * kVerifyWaves * sizeof(int64_t));
 }
 
 hipError_t launch_verify(int64_t B, int64_t T, int64_t V, const float* p, const float* q, const int32_t* tokens,

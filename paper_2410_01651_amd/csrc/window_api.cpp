@@ -45,7 +45,8 @@ gca_status check_rows(const gca_window* w) {
   GCA_TRY(check_ptr(w->v, "window v", true, 16));
   GCA_TRY(check_ptr(w->k_scale, "window k_scale", true, 4));
   GCA_TRY(check_ptr(w->v_scale, "window v_scale", true, 4));
-  return check_ptr(w->length, "window length", true, 4);
+  GCA_TRY(check_ptr(w->length, "window length", true, 4));
+  return check_ptr(w->ticket, "window ticket", true, 4);
 }
 
 // T new tokens of every sequence (bounds before products: B * H is at most 2^15).
@@ -93,7 +94,6 @@ gca_status gca_window_append(const gca_window* w, const void* k, const void* v, 
   GCA_TRY(check_window(w));
   GCA_TRY(check_tokens(w, T));
   GCA_TRY(check_rows(w));
-  GCA_TRY(check_ptr(w->ticket, "window ticket", true, 4));
   GCA_TRY(check_ptr(k, "k", true, 16));
   GCA_TRY(check_ptr(v, "v", true, 16));
   GCA_TRY(check_ptr(lengths, "lengths", false, 4));
@@ -110,7 +110,6 @@ gca_status gca_window_attn(const gca_window* w, const void* q, const int32_t* pa
   if (w->window > 0 && w->window + T - 1 > w->capacity)
     return fail(GCA_ERR_INVALID, "window + T - 1 must be <= capacity");
   GCA_TRY(check_rows(w));
-  GCA_TRY(check_ptr(w->ticket, "window ticket", true, 4));
   GCA_TRY(check_ptr(q, "q", true, 16));
   GCA_TRY(check_ptr(parents, "parents", false, 4));
   GCA_TRY(check_ptr(lengths, "lengths", false, 4));

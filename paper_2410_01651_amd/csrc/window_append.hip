@@ -18,7 +18,8 @@
 namespace gca {
 namespace {
 
-constexpr int kAppendWaves = 4;
+constexpr int kAppendWaves = 8;
+constexpr int64_t kFewTokens = 32;
 constexpr int kRingTile = kS * kD;  // bytes of a tile's keys or values
 
 struct AppendParams {
@@ -48,16 +49,98 @@ __device__ __forceinline__ int64_t new_tokens(const int32_t* lengths, uint32_t b
   return n < 0 ? 0 : n < T ? n : T;
 }
 
+// The largest magnitude of a lane's eight entries of a row, as its bits.
+__device__ __forceinline__ uint32_t top_of(const Row8<__bf16>& x) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;  // (magnitudes of bf16 order as integers)
+  u16x2 m = __builtin_bit_cast(u16x2, x.x[0] & 0x7fff7fffu);
+#pragma unroll
+  for (int c = 1; c < 4; ++c) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x.x[c] & 0x7fff7fffu));
+  return (uint32_t)max(m[0], m[1]) << 16;
+}
+__device__ __forceinline__ uint32_t top_of(const Row8<float>& x) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) top = max(top, __float_as_uint(x.at(c)) & 0x7fffffffu);
+  return top;
+}
+
+// A row's eight entries of this lane, of which `top` is the row's largest magnitude, as 8-bit numbers (w0, w1),
+// and the row's scale.
+template <bool I8, typename T>
+__device__ __forceinline__ float numbers_of(const Row8<T>& x, uint32_t top, bool values, uint32_t& w0, uint32_t& w1) {
+  const bool odd = top >= 0x7f800000u, nan = top > 0x7f800000u;  // anything not finite; NaN
+  if (__ballot(odd) != 0) {  // the largest finite magnitude
+    uint32_t fin = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t u = __float_as_uint(x.at(c)) & 0x7fffffffu;
+      fin = max(fin, u < 0x7f800000u ? u : 0u);
+    }
+    top = max_row8(fin);
+  }
+  float scale;
+  uint32_t w[2];
+  if constexpr (I8) {
+    const float amax = fmaxf(__uint_as_float(top), 0x1p-100f);
+    scale = amax / 127.f;
+    const float inv = 127.f / amax;  // |x| inv <= 127 (1 + 2 roundings): 127 at most once rounded
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      uint32_t o = 0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float y = x.at(4 * q + c) * inv;
+        if (odd) y = y == y ? fminf(fmaxf(y, -127.f), 127.f) : 0.f;
+        o |= ((uint32_t)(int)__builtin_rintf(y) & 0xffu) << (8 * c);
+      }
+      w[q] = o;
+    }
+  } else {
+    // 448 = 1.75 x 2^8: the least power of two s with amax / s <= 448 (at least 2^-126)
+    const int e = max((int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), 1);
+    scale = __uint_as_float((uint32_t)e << 23);
+    const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      uint32_t o = 0;
+#pragma unroll
+      for (int c = 0; c < 4; c += 2) {
+        float y0 = x.at(4 * q + c) * inv, y1 = x.at(4 * q + c + 1) * inv;
+        if (odd) {  // infinities (a comparison with NaN is false)
+          if (__builtin_fabsf(y0) > 448.f) y0 = __builtin_copysignf(448.f, y0);
+          if (__builtin_fabsf(y1) > 448.f) y1 = __builtin_copysignf(448.f, y1);
+          if (values) {  // (a value's number is never NaN: it would reach rows that do not see it)
+            y0 = y0 == y0 ? y0 : 0.f;
+            y1 = y1 == y1 ? y1 : 0.f;
+          }
+        }
+        o = pk_e4m3(y0, y1, o, c != 0);
+      }
+      w[q] = o;
+    }
+  }
+  w0 = w[0];
+  w1 = w[1];
+  return nan ? __builtin_nanf("") : scale;
+}
+
+// Tokens that are kept of the n new ones: [first, last).
+__device__ __forceinline__ int64_t first_kept(const AppendParams& p, int64_t n) {
+  return p.ring && n > p.C ? n - p.C : 0;
+}
+__device__ __forceinline__ int64_t last_kept(const AppendParams& p, int64_t length, int64_t n) {
+  return p.ring || length + n <= p.C ? n : p.C - length;
+}
+
+// Many tokens: one tile of rows.
 template <typename T, bool I8>
 __device__ __forceinline__ void append_tile(const AppendParams& p, uint32_t b, uint32_t item, int64_t length,
                                             int64_t n, int lane) {
   // item = (h tiles + t) 2 + which
   const uint32_t which = item & 1;
   const uint32_t h = __builtin_amdgcn_readfirstlane((item >> 1) / p.tiles), t = (item >> 1) - h * p.tiles;
-  // tokens that are kept: [i0, i1); the tile's: from position `first`
-  const int64_t i0 = p.ring && n > p.C ? n - p.C : 0;
-  const int64_t i1 = p.ring || length + n <= p.C ? n : p.C - length;
-  const int64_t first = ((length + i0) / kS + t) * kS;
+  const int64_t i0 = first_kept(p, n), i1 = last_kept(p, length, n);
+  const int64_t first = ((length + i0) / kS + t) * kS;  // the tile's first position
   int64_t lo = length + i0 - first, hi = length + i1 - first;  // its rows [lo, hi)
   lo = lo > 0 ? lo : 0;
   hi = hi < kS ? hi : kS;
@@ -75,66 +158,11 @@ __device__ __forceinline__ void append_tile(const AppendParams& p, uint32_t b, u
     const bool mine = row >= (int)lo && row < (int)hi;
     x[r].load(src, mine ? (uint32_t)((row - (int)lo) * kRow + cg * 8 * (int)sizeof(T)) : 0x40000000u, 0);
   }
-
   uint32_t w[16];  // row r: w[2 r], w[2 r + 1]
   float scale[8];
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) top = max(top, __float_as_uint(x[r].at(c)) & 0x7fffffffu);
-    top = max_row8(top);
-    const bool odd = top >= 0x7f800000u, nan = top > 0x7f800000u;
-    if (__any(odd)) {  // the largest finite magnitude
-      uint32_t fin = 0;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const uint32_t u = __float_as_uint(x[r].at(c)) & 0x7fffffffu;
-        fin = max(fin, u < 0x7f800000u ? u : 0u);
-      }
-      top = max_row8(fin);
-    }
-    if constexpr (I8) {
-      const float amax = fmaxf(__uint_as_float(top), 0x1p-100f);
-      scale[r] = amax / 127.f;
-      const float inv = 127.f / amax;  // |x| inv <= 127 (1 + 2 roundings): 127 at most once rounded
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        uint32_t o = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float y = x[r].at(4 * q + c) * inv;
-          if (odd) y = y == y ? fminf(fmaxf(y, -127.f), 127.f) : 0.f;
-          o |= ((uint32_t)(int)__builtin_rintf(y) & 0xffu) << (8 * c);
-        }
-        w[2 * r + q] = o;
-      }
-    } else {
-      // 448 = 1.75 x 2^8: the least power of two s with amax / s <= 448 (at least 2^-126)
-      const int e = max((int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), 1);
-      scale[r] = __uint_as_float((uint32_t)e << 23);
-      const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        uint32_t o = 0;
-#pragma unroll
-        for (int c = 0; c < 4; c += 2) {
-          float y0 = x[r].at(4 * q + c) * inv, y1 = x[r].at(4 * q + c + 1) * inv;
-          if (odd) {  // infinities (a comparison with NaN is false)
-            if (__builtin_fabsf(y0) > 448.f) y0 = __builtin_copysignf(448.f, y0);
-            if (__builtin_fabsf(y1) > 448.f) y1 = __builtin_copysignf(448.f, y1);
-            if (which) {  // (a value's number is never NaN: it would reach rows that do not see it)
-              y0 = y0 == y0 ? y0 : 0.f;
-              y1 = y1 == y1 ? y1 : 0.f;
-            }
-          }
-          o = pk_e4m3(y0, y1, o, c != 0);
-        }
-        w[2 * r + q] = o;
-      }
-    }
-    if (nan) scale[r] = __builtin_nanf("");
-  }
+  for (int r = 0; r < 8; ++r)
+    scale[r] = numbers_of<I8>(x[r], max_row8(top_of(x[r])), which, w[2 * r], w[2 * r + 1]);
 
   if (which) {
     // columns: w[2 c] holds rows 0-3 of column c, w[2 c + 1] rows 4-7
@@ -148,7 +176,7 @@ __device__ __forceinline__ void append_tile(const AppendParams& p, uint32_t b, u
 #pragma unroll
     for (int c = 0; c < 16; ++c) w[c] = o[c];
   }
-  const int64_t row0 = bh * p.C + (p.ring ? first % p.C : first);
+  const int64_t row0 = bh * p.C + (p.ring ? (uint32_t)first % (uint32_t)p.C : (uint32_t)first);  // (below 2^32)
   // keys: row 8 rg + r, bytes 8 cg ..; values: column 8 cg + r, bytes 8 rg ..
   uint8_t* dst = p.dst[which] + row0 * kD + (which ? cg * 8 * kS + rg * 8 : rg * 8 * kD + cg * 8);
   const int from = max((int)lo - 8 * rg, 0), to = min((int)hi - 8 * rg, 8);  // this lane's rows
@@ -169,32 +197,58 @@ __device__ __forceinline__ void append_tile(const AppendParams& p, uint32_t b, u
   if (cg >= from && cg < to) p.scale[which][row0 + 8 * rg + cg] = s;
 }
 
-// The last workgroup of a sequence to have read its length writes the new one: every workgroup takes a
-// ticket behind its read, and who takes the last knows that nobody reads any more.
+// Few tokens: eight of them, a lane for eight entries of one.  What is read does not depend on
+// the sequence's length, so it is asked for beside it.
 template <typename T, bool I8>
-__global__ __launch_bounds__(kAppendWaves * 64) void window_append_kernel(AppendParams p) {
-  __shared__ int32_t old;
+__device__ __forceinline__ void append_few(const AppendParams& p, uint32_t b, uint32_t item, int lane) {
+  // item = (h tiles + t) 2 + which: tokens 8 t ..
+  const uint32_t which = item & 1;
+  const uint32_t h = __builtin_amdgcn_readfirstlane((item >> 1) / p.tiles), t = (item >> 1) - h * p.tiles;
+  const int cg = lane & 7;
+  const int64_t i = 8 * t + (lane >> 3), bh = (int64_t)b * p.Hkv + h;
+  constexpr int kRow = kD * (int)sizeof(T);
+  Row8<T> x;
+  x.load(range_rsrc(reinterpret_cast<const char*>(p.src[which]) + bh * p.T * kRow, (uint32_t)(p.T * kRow)),
+         (uint32_t)(i * kRow + cg * 8 * (int)sizeof(T)), 0);
+  const int64_t length = max(p.length[b], 0), n = new_tokens(p.lengths, b, p.T);
+  uint32_t w0, w1;
+  const float scale = numbers_of<I8>(x, max_row8(top_of(x)), which, w0, w1);
+  if (i < first_kept(p, n) || i >= last_kept(p, length, n)) return;
+  const uint32_t pos = (uint32_t)length + (uint32_t)i, row = p.ring ? pos % (uint32_t)p.C : pos;
+  if (which) {
+    uint8_t* dst = p.dst[1] + (bh * p.C + (row & ~63u)) * kD + cg * 8 * kS + (row & 63u);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) dst[c * kS] = (uint8_t)((c < 4 ? w0 : w1) >> (8 * (c & 3)));
+  } else {
+    *reinterpret_cast<u32x2*>(p.dst[0] + (bh * p.C + row) * kD + cg * 8) = u32x2{w0, w1};
+  }
+  if (cg == 0) p.scale[which][bh * p.C + row] = scale;
+}
+
+// Whoever takes a sequence's last ticket knows that every workgroup has read its length, and writes
+// the new one.  (A workgroup takes its ticket once its waves have read, at its end, when nothing waits for it.)
+__device__ __forceinline__ void update_length(int32_t* length, int32_t* ticket, int32_t per, int64_t now) {
+  bool last = per == 1;
+  if (!last) {
+    last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == per - 1;
+    if (last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (last) *length = (int32_t)(now < 0x7fffffff ? now : 0x7fffffff);
+}
+
+template <typename T, bool I8, bool FEW>
+__global__ __launch_bounds__(FEW ? 1024 : kAppendWaves * 64) void window_append_kernel(AppendParams p) {
   const uint32_t b = blockIdx.x / p.per, part = blockIdx.x - b * p.per;
-  int32_t drawn = 0;
-  if (threadIdx.x == 0) {
-    int32_t len = p.length[b];
-    old = len;
-    if (p.per > 1) {
-      asm volatile("" : "+v"(len)::"memory");  // (the value is here before the ticket is asked for)
-      drawn = __hip_atomic_fetch_add(p.ticket + (int64_t)b * p.stride, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-  }
-  __syncthreads();
-  const int64_t length = max(old, 0);
-  const int64_t n = new_tokens(p.lengths, b, p.T);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t item = part * kAppendWaves + wave;
-  if (item < p.items) append_tile<T, I8>(p, b, item, length, n, threadIdx.x & 63);
-  if (threadIdx.x == 0 && drawn == (int32_t)p.per - 1) {
-    const int64_t len = length + n;
-    p.length[b] = (int32_t)(len < 0x7fffffff ? len : 0x7fffffff);
-    if (p.per > 1) __hip_atomic_store(p.ticket + (int64_t)b * p.stride, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const uint32_t waves = blockDim.x >> 6;
+  const int64_t length = max((int)__builtin_amdgcn_readfirstlane(p.length[b]), 0);
+  const int64_t n = new_tokens(p.lengths, b, p.T);
+  for (uint32_t item = part * waves + wave; item < p.items; item += p.per * waves) {
+    if constexpr (FEW) append_few<T, I8>(p, b, item, threadIdx.x & 63);
+    else append_tile<T, I8>(p, b, item, length, n, threadIdx.x & 63);
   }
+  __syncthreads();  // (the workgroup's waves have read the length)
+  if (threadIdx.x == 0) update_length(p.length + b, p.ticket + (int64_t)b * p.stride, (int32_t)p.per, length + n);
 }
 
 struct KeepParams {
@@ -203,62 +257,65 @@ struct KeepParams {
   float* ks;
   float* vs;
   int32_t* length;
+  int32_t* ticket;
   const int32_t* path;
   const int32_t* lengths;
   int64_t T, C;
-  uint32_t Hkv, n;
+  uint32_t Hkv, n, per, stride;
   int ring;
 };
 
-constexpr int kKeepWaves = 8;
+constexpr int kKeepWaves = 4;
+constexpr int kKeepTokens = 8;  // at a time
 
-// One workgroup per sequence, its waves taking the cached heads in turn.
+// One wave per (sequence, cached head).
 __global__ __launch_bounds__(kKeepWaves * 64) void window_keep_kernel(KeepParams p) {
-  const uint32_t b = blockIdx.x;
+  const uint32_t b = blockIdx.x / p.per, part = blockIdx.x - b * p.per;
   const int lane = threadIdx.x & 63;
+  const int length = max((int)__builtin_amdgcn_readfirstlane(p.length[b]), 0);
   const int64_t n = new_tokens(p.lengths, b, p.T);
-  const int64_t length = max(p.length[b], 0);
   // lane i: entry i, in the path if every entry up to it is larger than the one before
   const int mine = lane < (int)p.n ? p.path[(int64_t)b * p.n + lane] : -1;
   const int left = __shfl_up(mine, 1);  // (by every lane: one that is not active has nothing to give)
   const uint64_t good = __ballot(mine > (lane ? left : -1) && mine < n);
   const int m = good == ~0ull ? 64 : __builtin_ctzll(~good);
-  __syncthreads();  // every wave has read the length
   const int64_t base = length > n ? length - n : 0;
-  if (threadIdx.x == 0) p.length[b] = (int32_t)(base + m);
+  const uint32_t h = part * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // entries that name their own place lead the path and stay
   const uint64_t moved = __ballot(lane < m && mine != lane);
-  if (moved == 0) return;
-  const int first = __builtin_ctzll(moved);
-  auto row_of = [&](int64_t pos) { return p.ring ? pos % p.C : pos; };
-  for (uint32_t h = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); h < p.Hkv; h += kKeepWaves) {
+  if (moved != 0 && h < p.Hkv) {
     const int64_t row0 = ((int64_t)b * p.Hkv + h) * p.C;
-    // four tokens at a time: all that they come from is read before any is written
-    for (int i = first; i < m; i += 4) {
-      uint8_t kb[4], vb[4];
-      float sc[4];
-      int64_t to[4];
+    // lane i: the rows that entry i comes from and goes to (-1: one is past the capacity); positions are below 2^32
+    const uint32_t C = (uint32_t)p.C, src = (uint32_t)base + (uint32_t)mine, dst = (uint32_t)base + (uint32_t)lane;
+    int from = (int)(p.ring ? src % C : src), to = (int)(p.ring ? dst % C : dst);
+    if (lane >= m || (!p.ring && (src >= C || dst >= C))) from = to = -1;
+    for (int i = __builtin_ctzll(moved); i < m; i += kKeepTokens) {
+      // all that these tokens come from is read before any is written (a descriptor that is empty where
+      // there is no token: nothing is asked for)
+      uint8_t kb[kKeepTokens], vb[kKeepTokens];
+      float sc[kKeepTokens];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int at = min(i + e, m - 1);
-        const int64_t from = row_of(base + __builtin_amdgcn_readlane(mine, at));
-        to[e] = row_of(base + at);
-        // (a row past the capacity is neither there nor wanted)
-        if (i + e >= m || from >= p.C || to[e] >= p.C) to[e] = -1;
-        const int64_t f = to[e] < 0 ? 0 : from;
-        kb[e] = p.k[(row0 + f) * kD + lane];
-        vb[e] = p.v[(row0 + (f & ~63)) * kD + lane * kS + (f & 63)];
-        sc[e] = lane < 2 ? (lane ? p.vs : p.ks)[row0 + f] : 0.f;
+      for (int e = 0; e < kKeepTokens; ++e) {
+        const int f = i + e < m ? __builtin_amdgcn_readlane(from, min(i + e, 63)) : -1;
+        const int64_t r = row0 + max(f, 0);
+        const char* const k = reinterpret_cast<const char*>(p.k) + r * kD;
+        const char* const v = reinterpret_cast<const char*>(p.v) + (r & ~(int64_t)63) * kD + (r & 63);
+        kb[e] = __builtin_amdgcn_raw_buffer_load_b8(range_rsrc(k, f < 0 ? 0 : kD), lane, 0, 0);
+        vb[e] = __builtin_amdgcn_raw_buffer_load_b8(range_rsrc(v, f < 0 ? 0 : kD * kS), lane * kS, 0, 0);
+        sc[e] = (lane & 1 ? p.vs : p.ks)[r];
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (to[e] < 0) continue;
-        p.k[(row0 + to[e]) * kD + lane] = kb[e];
-        p.v[(row0 + (to[e] & ~63)) * kD + lane * kS + (to[e] & 63)] = vb[e];
-        if (lane < 2) (lane ? p.vs : p.ks)[row0 + to[e]] = sc[e];
+      for (int e = 0; e < kKeepTokens; ++e) {
+        const int t = i + e < m ? __builtin_amdgcn_readlane(to, min(i + e, 63)) : -1;
+        if (t < 0) continue;
+        p.k[(row0 + t) * kD + lane] = kb[e];
+        p.v[(row0 + (t & ~63)) * kD + lane * kS + (t & 63)] = vb[e];
+        if (lane < 2) (lane & 1 ? p.vs : p.ks)[row0 + t] = sc[e];
       }
     }
   }
+  __syncthreads();  // (the workgroup's waves have read the length)
+  if (threadIdx.x == 0) update_length(p.length + b, p.ticket + (int64_t)b * p.stride, (int32_t)p.per, base + m);
 }
 
 }  // namespace
@@ -278,20 +335,28 @@ hipError_t launch_window_append(const gca_window& w, const void* k, const void* 
   p.T = T;
   p.C = w.capacity;
   p.seqs = (uint32_t)w.B;
-  p.tiles = (uint32_t)tiles_of(T < w.capacity ? T : w.capacity);
+  const bool few = T <= kFewTokens;
+  p.tiles = (uint32_t)(few ? (T + 7) / 8 : tiles_of(T < w.capacity ? T : w.capacity));
   p.Hkv = (uint32_t)w.Hkv;
   p.stride = 2 * (uint32_t)w.H;
   p.items = p.Hkv * p.tiles * 2;
-  p.per = (p.items + kAppendWaves - 1) / kAppendWaves;
+  // few tokens: as many waves per workgroup as go, so that one may do for a sequence and needs no ticket
+  const uint32_t waves = few ? (p.items < 16 ? p.items : 16) : kAppendWaves;
+  p.per = (p.items + waves - 1) / waves;
+  if (!few) {  // no more workgroups than run at once: every one takes a ticket
+    const uint32_t most = 2 * (uint32_t)device_cus() / p.seqs;
+    if (p.per > most) p.per = most > 1 ? most : 1;
+  }
   p.ring = w.window > 0;
-  const dim3 grid(p.seqs * p.per), block(kAppendWaves * 64);
-  const bool i8 = w.format == GCA_INT8;
-  if (w.dtype == GCA_BF16)
-    launch_kernel("window_append_kernel", i8 ? window_append_kernel<__bf16, true> : window_append_kernel<__bf16, false>,
+  const dim3 grid(p.seqs * p.per), block(waves * 64);
+  auto run = [&](auto tag, auto i8) {
+    using E = decltype(tag);
+    constexpr bool I8 = decltype(i8)::value;
+    launch_kernel("window_append_kernel", few ? window_append_kernel<E, I8, true> : window_append_kernel<E, I8, false>,
                   grid, block, 0, stream, p);
-  else
-    launch_kernel("window_append_kernel", i8 ? window_append_kernel<float, true> : window_append_kernel<float, false>,
-                  grid, block, 0, stream, p);
+  };
+  if (w.dtype == GCA_BF16) w.format == GCA_INT8 ? run(__bf16{}, std::true_type{}) : run(__bf16{}, std::false_type{});
+  else w.format == GCA_INT8 ? run(float{}, std::true_type{}) : run(float{}, std::false_type{});
   return take_launch_error();
 }
 
@@ -309,8 +374,12 @@ hipError_t launch_window_keep(const gca_window& w, const int32_t* path, int64_t 
   p.C = w.capacity;
   p.Hkv = (uint32_t)w.Hkv;
   p.n = (uint32_t)n;
+  p.ticket = w.ticket;
+  p.stride = 2 * (uint32_t)w.H;
+  const uint32_t waves = p.Hkv < kKeepWaves ? p.Hkv : kKeepWaves;
+  p.per = (p.Hkv + waves - 1) / waves;
   p.ring = w.window > 0;
-  launch_kernel("window_keep_kernel", window_keep_kernel, dim3((unsigned)w.B), dim3(kKeepWaves * 64), 0, stream, p);
+  launch_kernel("window_keep_kernel", window_keep_kernel, dim3((unsigned)w.B * p.per), dim3(waves * 64), 0, stream, p);
   return take_launch_error();
 }
 

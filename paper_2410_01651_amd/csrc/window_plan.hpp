@@ -28,7 +28,7 @@ size_t window_workspace(const gca_window& w, int64_t T);
 
 struct VerifyPlan {
   int64_t slices;  // of the vocabulary, per sequence
-  int64_t per;     // entries of a slice
+  int64_t per;     // entries of one wave of a slice
 };
 VerifyPlan verify_plan(int64_t B, int64_t V);
 size_t verify_workspace(int64_t B, int64_t T, int64_t V);

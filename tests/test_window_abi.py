@@ -85,7 +85,7 @@ def test_malformed_window_is_refused(gca, field, value, status):
 
 @pytest.mark.parametrize("call,names", [
     (_append, ("k", "v", "k_scale", "v_scale", "length", "ticket")), (_attn, ("k", "v", "k_scale", "v_scale", "length", "ticket")),
-    (_keep, ("k", "v", "k_scale", "v_scale", "length"))])
+    (_keep, ("k", "v", "k_scale", "v_scale", "length", "ticket"))])
 def test_missing_members_are_refused(gca, call, names):
     for name in names:
         assert call(gca, _window(gca, **{name: None})) == gca.GCA_ERR_INVALID
