@@ -74,6 +74,17 @@ __device__ __forceinline__ f16x8 to_f16(uint32_t x, uint32_t y) {
   }
 }
 
+// Eight e4m3 numbers times 2^-9 as an fp16 operand (below 1, and exact).
+__device__ __forceinline__ f16x8 to_f16_small(uint32_t x, uint32_t y) {
+  constexpr float k = 0x1p-9f;
+  const u32x4 r = u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, k, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, k, true)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y, k, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y, k, true))};
+  return __builtin_bit_cast(f16x8, r);
+}
+
 __device__ __forceinline__ void store8(__bf16* p, const float* x) {
   bf16x8 r;
 #pragma unroll

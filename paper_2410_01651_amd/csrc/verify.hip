@@ -173,23 +173,37 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* lds) {
   for (int w = 0; w < kVerifyWaves; ++w) s += lds[w];
   return s;
 }
+// Sum of the threads up to this one, and of all.
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* lds, int64_t& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const int64_t y = __shfl_up(x, s);
+    if (lane >= s) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) lds[wave] = x;
+  __syncthreads();
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kVerifyWaves; ++w) {
+    if (w < wave) x += lds[w];
+    all += lds[w];
+  }
+  return x;
+}
 
-__global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParams p) {
-  __shared__ Walk w;
-  __shared__ int64_t lds[kVerifyWaves];
-  __shared__ int again;
-  const uint32_t b = blockIdx.x / p.slices, slice = blockIdx.x - b * p.slices;
+// The walk of sequence b into w, by the whole workgroup.
+__device__ __forceinline__ void walk_tree(const VerifyParams& p, uint32_t b, Walk& w, int& again, int64_t* lds) {
   const int lane = threadIdx.x & 63;
   const bool first_wave = threadIdx.x < 64, drawn = p.q != nullptr;
 
   // lane i: node i
-  int n = p.lengths ? p.lengths[b] : (int)p.T;
-  n = max(min(n, (int)p.T), 0);
   int par = -1, tok = -1;
   float u = 0.f;
   double r = 0.0, q = 0.0;
   bool real = false;  // a token of the vocabulary
-  if (first_wave && lane < n) {
+  if (first_wave && lane < (int)p.T) {  // (of every node: not to wait for their number)
     const int64_t at = (int64_t)b * p.T + lane;
     par = p.parents ? p.parents[at] : lane - 1;
     if (par >= lane) par = -1;
@@ -203,6 +217,9 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
       q = drawn ? prob(p.q[e]) : 1.0;
     }
   }
+  int n = p.lengths ? p.lengths[b] : (int)p.T;
+  n = max(min(n, (int)p.T), 0);
+  real = real && lane < n;
   int cur = n > 0 ? 0 : -1, rejected = 0;
   uint64_t on = n > 0 ? 1 : 0, done = 0;  // accepted nodes; tested ones
   double z = 1.0;
@@ -273,15 +290,28 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
     z = (double)s * kUnfix;
     __syncthreads();  // (`again` and the walk are read before they are written again)
   }
+}
 
+// The walk's outputs.
+__device__ __forceinline__ void write_path(const VerifyParams& p, uint32_t b, const Walk& w) {
+  const int lane = threadIdx.x;
+  if (lane >= (int)p.T) return;  // entry i of the path is the i-th node of the walk
+  const int64_t at = (int64_t)b * p.T;
+  const int count = __builtin_popcountll(w.on);
+  if (w.on >> lane & 1) p.path[at + __builtin_popcountll(w.on & ((1ull << lane) - 1))] = lane;
+  if (lane >= count) p.path[at + lane] = -1;
+  if (lane == 0) p.count[b] = count;
+}
+
+__global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParams p) {
+  __shared__ Walk w;
+  __shared__ int64_t lds[kVerifyWaves];
+  __shared__ int again;
+  const uint32_t b = blockIdx.x / p.slices, slice = blockIdx.x - b * p.slices;
+  const int lane = threadIdx.x & 63;
+  walk_tree(p, b, w, again, lds);
   if (slice == 0) {
-    if (first_wave && lane < (int)p.T) {  // entry i of the path is the i-th node of the walk
-      const int64_t at = (int64_t)b * p.T;
-      const int count = __builtin_popcountll(on);
-      if (on >> lane & 1) p.path[at + __builtin_popcountll(on & ((1ull << lane) - 1))] = lane;
-      if (lane >= count) p.path[at + lane] = -1;
-      if (lane == 0) p.count[b] = count;
-    }
+    write_path(p, b, w);
     const int words = sizeof(Walk) / 4;
     for (int x = threadIdx.x; x < words; x += kVerifyThreads)
       reinterpret_cast<uint32_t*>(p.walk + b)[x] = reinterpret_cast<const uint32_t*>(&w)[x];
@@ -294,58 +324,97 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
   if (lane == 0) p.sums[(int64_t)b * p.slices * kVerifyWaves + quarter] = s;
 }
 
-// One workgroup per sequence: the slice that the drawn place is in, and the token in it.
+// The first entry of [lo, hi) of the last node's row whose partial sum from lo on exceeds `place`; `plain`: of
+// p[a] itself.  kPerThread consecutive entries per thread.
+__device__ __forceinline__ void draw(const VerifyParams& p, const Walk& w, uint32_t b, uint32_t lo, uint32_t hi,
+                                     int64_t place, bool plain, int64_t* lds) {
+  const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
+  const bool drawn = p.q != nullptr && w.rejected > 0;
+  const float* pr = p.p + row;
+  const float* qr = drawn ? p.q + row : pr;
+  int64_t before = 0;
+  for (uint32_t x0 = lo; x0 < hi; x0 += kVerifyThreads * kPerThread) {
+    const uint32_t x = x0 + threadIdx.x * kPerThread;
+    float pe[kPerThread], qe[kPerThread];
+    if (x + kPerThread <= p.V) {
+#pragma unroll
+      for (int e = 0; e < kPerThread; e += 4) {
+        const f32x4u a = *reinterpret_cast<const f32x4u*>(pr + x + e), c = *reinterpret_cast<const f32x4u*>(qr + x + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          pe[e + i] = a[i];
+          qe[e + i] = c[i];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kPerThread; ++e) {
+        pe[e] = x + e < p.V ? pr[x + e] : 0.f;
+        qe[e] = x + e < p.V ? qr[x + e] : 0.f;
+      }
+    }
+    int64_t r[kPerThread], mine = 0;
+    left<kPerThread>(w, drawn && !plain, p.q == nullptr && !plain, pe, qe, x, r);
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) {
+      r[e] = x + e < hi ? r[e] : 0;
+      mine += r[e];
+    }
+    int64_t step;
+    const int64_t upto = before + block_scan(mine, lds, step);
+    if (upto > place && upto - mine <= place) {  // one thread
+      int64_t at = upto - mine;
+      uint32_t found = x;
+#pragma unroll
+      for (int e = 0; e < kPerThread; ++e) {
+        at += r[e];
+        if (at <= place) found = x + e + 1;
+      }
+      p.next[b] = (int32_t)found;
+    }
+    before += step;
+    if (before > place) break;  // (uniform)
+  }
+}
+
+// One workgroup per sequence, from what the walk's launch left: the part that the drawn place is in, four sums
+// per thread, and the token in it.
 __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParams p) {
   __shared__ Walk w;
   __shared__ int64_t lds[kVerifyWaves];
-  __shared__ int64_t place;  // in the slice
+  __shared__ int64_t place;
   __shared__ uint32_t chosen;
-  const uint32_t b = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63;
-  for (int x = tid; x < (int)(sizeof(Walk) / 4); x += kVerifyThreads)
-    reinterpret_cast<uint32_t*>(&w)[x] = reinterpret_cast<const uint32_t*>(p.walk + b)[x];
+  const uint32_t b = blockIdx.x, tid = threadIdx.x;
   float u = p.u[(int64_t)b * p.T];
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+  int64_t part[kVerifyWaves];
+#pragma unroll
+  for (int e = 0; e < kVerifyWaves; ++e)
+    part[e] = tid < p.slices ? p.sums[((int64_t)b * p.slices + tid) * kVerifyWaves + e] : 0;
+  if (tid < sizeof(Walk) / 4) reinterpret_cast<uint32_t*>(&w)[tid] = reinterpret_cast<const uint32_t*>(p.walk + b)[tid];
+  static_assert(sizeof(Walk) / 4 <= kVerifyThreads, "one word per thread");
   __syncthreads();
   if (w.node < 0) {
     if (tid == 0) p.next[b] = -1;
     return;
   }
-  const bool drawn = p.q != nullptr;
-  // (four sums per thread, its slice's)
-  int64_t part[kVerifyWaves], mine = 0;
+  int64_t mine = 0, total;
 #pragma unroll
-  for (int e = 0; e < kVerifyWaves; ++e) {
-    part[e] = tid < (int)p.slices ? p.sums[((int64_t)b * p.slices + tid) * kVerifyWaves + e] : 0;
-    mine += part[e];
-  }
-  bool plain = false;
-  int64_t upto = mine;  // sum of the slices up to this one
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) {
-    const int64_t y = __shfl_up(upto, s);
-    if (lane >= s) upto += y;
-  }
-  if (lane == 63) lds[tid >> 6] = upto;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int y = 0; y < kVerifyWaves; ++y) {
-    if (y < (tid >> 6)) upto += lds[y];
-    total += lds[y];
-  }
+  for (int e = 0; e < kVerifyWaves; ++e) mine += part[e];
+  const int64_t upto = block_scan(mine, lds, total);
   uint32_t lo = 0, hi = p.V;
-  if (total == 0) {  // nothing is left: of p itself, the whole vocabulary as one slice
+  bool plain = false;
+  int64_t at;
+  if (total == 0) {  // nothing is left: of p itself, the whole vocabulary as one part
     plain = true;
-    total = block_sum(part_sum(p, w, b, 0, p.V, true, threadIdx.x, kVerifyThreads), lds);
+    total = block_sum(part_sum(p, w, b, 0, p.V, true, tid, kVerifyThreads), lds);
     if (total == 0) {
       if (tid == 0) p.next[b] = -1;
       return;
     }
-    if (tid == 0) place = (int64_t)((double)u * (double)total);
-    __syncthreads();
+    at = (int64_t)((double)u * (double)total);
   } else {
-    int64_t at = (int64_t)((double)u * (double)total);
+    at = (int64_t)((double)u * (double)total);
     if (upto > at && upto - mine <= at) {  // one thread
       at -= upto - mine;
       uint32_t e = 0;
@@ -361,70 +430,9 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParam
     __syncthreads();
     lo = chosen * p.per;
     hi = min(lo + p.per, p.V);
+    at = place;
   }
-  // blocks of entries in order, kPerThread consecutive ones per thread
-  const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
-  const float* pr = p.p + row;
-  const float* qr = drawn && w.rejected > 0 ? p.q + row : pr;
-  int64_t before = 0;
-  for (uint32_t x0 = lo; x0 < hi; x0 += kVerifyThreads * kPerThread) {
-    const uint32_t x = x0 + tid * kPerThread;
-    f32x4u a[kPerThread / 4], c[kPerThread / 4];
-    if (x + kPerThread <= p.V) {
-#pragma unroll
-      for (int e = 0; e < kPerThread / 4; ++e) {
-        a[e] = *reinterpret_cast<const f32x4u*>(pr + x + 4 * e);
-        c[e] = *reinterpret_cast<const f32x4u*>(qr + x + 4 * e);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < kPerThread; ++e) {
-        a[e / 4][e % 4] = x + e < p.V ? pr[x + e] : 0.f;
-        c[e / 4][e % 4] = x + e < p.V ? qr[x + e] : 0.f;
-      }
-    }
-    float pe[kPerThread], qe[kPerThread];
-    int64_t r[kPerThread], mine = 0;
-#pragma unroll
-    for (int e = 0; e < kPerThread; ++e) {
-      pe[e] = a[e / 4][e % 4];
-      qe[e] = c[e / 4][e % 4];
-    }
-    left<kPerThread>(w, drawn && !plain, !plain, pe, qe, x, r);
-#pragma unroll
-    for (int e = 0; e < kPerThread; ++e) {
-      r[e] = x + e < hi ? r[e] : 0;
-      mine += r[e];
-    }
-    int64_t upto = mine;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      const int64_t y = __shfl_up(upto, s);
-      if (lane >= s) upto += y;
-    }
-    __syncthreads();
-    if (lane == 63) lds[tid >> 6] = upto;
-    __syncthreads();
-    int64_t step = 0;
-#pragma unroll
-    for (int y = 0; y < kVerifyWaves; ++y) {
-      if (y < (tid >> 6)) upto += lds[y];
-      step += lds[y];
-    }
-    upto += before;
-    if (upto > place && upto - mine <= place) {  // one thread
-      int64_t at = upto - mine;
-      uint32_t found = x;
-#pragma unroll
-      for (int e = 0; e < kPerThread; ++e) {
-        at += r[e];
-        if (at <= place) found = x + e + 1;
-      }
-      p.next[b] = (int32_t)found;
-    }
-    before += step;
-    if (before > place) break;  // (uniform)
-  }
+  draw(p, w, b, lo, hi, at, plain, lds);
 }
 
 }  // namespace
@@ -444,7 +452,8 @@ VerifyPlan verify_plan(int64_t B, int64_t V) {
 
 size_t verify_workspace(int64_t B, int64_t T, int64_t V) {
   (void)T;
-  return align256((size_t)B * sizeof(Walk)) + align256((size_t)B * verify_plan(B, V).slices * kVerifyWaves * sizeof(int64_t));
+  const VerifyPlan a = verify_plan(B, V);
+  return align256((size_t)B * sizeof(Walk)) + align256((size_t)B * a.slices * kVerifyWaves * sizeof(int64_t));
 }
 
 hipError_t launch_verify(int64_t B, int64_t T, int64_t V, const float* p, const float* q, const int32_t* tokens,

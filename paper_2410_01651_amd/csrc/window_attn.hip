@@ -53,6 +53,7 @@ struct WindowParams {
   float* lse;
   float* part;    // partial results of split row blocks: [item][row][64], then [item][row][2]
   float* part_ml;
+  int32_t* ticket;  // [row block]: the last workgroup joins the parts; null: window_join_kernel does
   float scale;    // |attn_scale| log2 e (log2 e where attn_scale is 0)
   float unscale;  // 1 / |attn_scale| (1)
   uint32_t negate, keep;  // xor and and masks of one query entry (fp32) or two: the scale's sign, and zero
@@ -72,11 +73,64 @@ __device__ __forceinline__ Joined finish(float m, float l, int off_by_one) {
   return Joined{m, l};
 }
 
+// Parts of a split row block go through memory that every XCD sees: two floats written and read past the
+// caches that each XCD has for itself.
+__device__ __forceinline__ void put2(float* at, float x, float y) {
+  const uint64_t u = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(at), u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 get2(const float* at) {
+  const uint64_t u = __hip_atomic_load(reinterpret_cast<const uint64_t*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return f32x2{__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))};
+}
+
+// Joins the parts of a split row block: columns 4 x .. of its row m, row r0 + m of the output.
+template <typename T, int QB, uint32_t kAhead>  // kAhead: parts asked for at a time
+__device__ __forceinline__ void join_rows_by(const WindowParams& p, uint32_t bb, uint32_t m, uint32_t x, int64_t r0) {
+  float top = kLowest, l = 0.f;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (uint32_t s0 = 0; s0 < p.splits; s0 += kAhead) {
+    f32x2 ml[kAhead], a[kAhead], c[kAhead];
+#pragma unroll
+    for (uint32_t s = 0; s < kAhead; ++s) {
+      const int64_t at = ((int64_t)bb * p.splits + min(s0 + s, p.splits - 1)) * QB + m;
+      ml[s] = get2(p.part_ml + at * 2);
+      a[s] = get2(p.part + at * kD + 4 * x);
+      c[s] = get2(p.part + at * kD + 4 * x + 2);
+    }
+    float now = top;
+#pragma unroll
+    for (uint32_t s = 0; s < kAhead; ++s) now = fmaxf(now, ml[s][0]);  // (the last part's again does no harm)
+    const float shrink = __builtin_amdgcn_exp2f(top - now);
+    l *= shrink;
+    acc *= shrink;
+    top = now;
+#pragma unroll
+    for (uint32_t s = 0; s < kAhead; ++s) {
+      if (s0 + s >= p.splits || ml[s][1] == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[s][0] - top);
+      l = fmaf(ml[s][1], f, l);
+      acc += f32x4{a[s][0], a[s][1], c[s][0], c[s][1]} * f;
+    }
+  }
+  const Joined j = finish(top, l, p.off_by_one);
+  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
+  const int64_t r = r0 + m;
+  store4(reinterpret_cast<T*>(p.out) + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
+  if (p.lse && x == 0) p.lse[r] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+}
+
+template <typename T, int QB>
+__device__ __forceinline__ void join_rows(const WindowParams& p, uint32_t bb, uint32_t m, uint32_t x, int64_t r0) {
+  if (p.splits <= 4) join_rows_by<T, QB, 2>(p, bb, m, x, r0);
+  else join_rows_by<T, QB, 8>(p, bb, m, x, r0);
+}
+
 // (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
 // floating point flags and would be called.)
 // T: type of the queries; W: MFMA tile; NC: column blocks of W query rows.
 template <typename T, bool I8, int W, int NC>
-__global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowParams p) {
+__global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) void window_attn_kernel(WindowParams p) {
   constexpr bool kB16 = sizeof(T) == 2;
   constexpr int NG = 64 / W;           // lane groups
   constexpr int NA = 64 / W;           // blocks of W tokens (or columns) per tile
@@ -87,6 +141,9 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   constexpr int QP = kB16 ? 1 : 3;     // bf16 terms of a query entry
   constexpr int PP = kB16 ? 1 : 2;     // fp16 terms of a probability
   constexpr int QB = W * NC;           // query rows per item
+  // Values take their scales along (e4m3: powers of two, so exactly) where two column blocks share them; else
+  // the probabilities do, which are then fewer.
+  constexpr bool VS = !I8 && kB16 && NC == 2;
   typedef __attribute__((ext_vector_type(NR))) float Acc;
   extern __shared__ __attribute__((aligned(16))) float smem[];
 
@@ -139,28 +196,22 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
 
   // ---- this lane's rows
   uint32_t row[NC];    // of the group
+  int token[NC];
   int depth[NC];       // position - base
-  uint64_t sees[NC];   // tree: new tokens it sees
-  uint64_t above[NC];  // tree: its ancestors and itself
   float slope[NC];     // in units of a score before its scale
-  bool live[NC];
+  // a node's ancestors and itself
+  auto above = [&](int i) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * i, (int)(uint32_t)up);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * i, (int)(uint32_t)(up >> 32));
+    return (uint64_t)hi << 32 | lo;
+  };
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const uint32_t m = m0 + min((uint32_t)(c * W + col), nrows - 1);
     const uint32_t gh = m / p.T, t = m - gh * p.T;
     row[c] = m;
-    depth[c] = (int)t;
-    live[c] = (uint32_t)(c * W + col) < nrows && (int)t < n;
-    above[c] = sees[c] = 0;
-    if (p.parents) {
-      const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (int)t, (int)(uint32_t)up);
-      const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (int)t, (int)(uint32_t)(up >> 32));
-      above[c] = (uint64_t)hi << 32 | lo;
-      depth[c] = __builtin_popcountll(above[c]) - 1;
-      sees[c] = above[c];
-      if (p.window)  // ancestors `window` levels up or more
-        for (int x = depth[c] - p.window; x >= 0; --x) sees[c] &= sees[c] - 1;
-    }
+    token[c] = depth[c] = (int)t;
+    if (p.parents) depth[c] = __builtin_popcountll(above((int)t)) - 1;
     slope[c] = p.slopes ? p.slopes[h * p.G + gh] * p.unscale : 0.f;
   }
 
@@ -199,11 +250,11 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
         range_rsrc(reinterpret_cast<const char*>(from + (head_tiles + s) * kS), there ? kS * 4 : 0), lane * 4, 0, 0));
   };
 
-  int t = t0 + (int)me;
+  int t = t1 - 1 - (int)me;  // (from the newest on: with biases the maximum is there, and stays)
   u32x4 kr[NA * NX], vr[NA * NX];
   float ksc, vsc;
   {
-    const bool there = t < t1;
+    const bool there = t >= t0;
     const uint32_t s = there ? slot(t) : 0;
     load_tile(kr, p.k, s, there);
     ksc = load_scale(p.ks, s, there);
@@ -253,10 +304,10 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     for (int a = 0; a < NA; ++a) o[c][a] = Acc{};
   }
 
-  for (; t < t1; t += (int)workers) {
+  for (; t >= t0; t -= (int)workers) {
     const int p0 = t << 6;  // the tile's first position
-    const int tn = t + (int)workers;
-    const bool more = tn < t1;
+    const int tn = t - (int)workers;
+    const bool more = tn >= t0;
     const uint32_t sn = more ? slot(tn) : 0;
 
     // scales, those of values over u: tokens that nobody sees have none
@@ -274,7 +325,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     }
     wave_lds_order();
     sc_lds[lane] = ksc;
-    sc_lds[64 + lane] = __builtin_ldexpf(nu, 15 - octave);  // at most 2^15
+    const float nu15 = __builtin_ldexpf(nu, 15 - octave);  // at most 2^15
+    // values whose scale is NaN: none here, their tokens' probabilities become NaN in the rows that see them
+    const uint64_t bad = __ballot((__float_as_uint(nu) & 0x7fffffffu) > 0x7f800000u);
+    const float mine = bad >> lane & 1 ? 0.f : nu15;
+    if constexpr (VS) reinterpret_cast<_Float16*>(sc_lds + 64)[lane] = (_Float16)mine;
+    else sc_lds[64 + lane] = mine;
     wave_lds_order();
 
     // S^T = N Q^T
@@ -325,7 +381,10 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
         if (p.parents) {
           mask = off >= 64 ? ~0ull : off > 0 ? (1ull << off) - 1 : 0ull;
           mask = lo < 64 ? mask & (~0ull << lo) : 0ull;
-          if (off < 64) mask |= off >= 0 ? sees[c] << off : off > -64 ? sees[c] >> -off : 0ull;
+          uint64_t sees = above(token[c]);
+          if (p.window)  // without ancestors `window` levels up or more
+            for (int x = depth[c] - p.window; x >= 0; --x) sees &= sees - 1;
+          if (off < 64) mask |= off >= 0 ? sees << off : off > -64 ? sees >> -off : 0ull;
         } else {
           const int hi = off + depth[c];  // the row's own
           mask = lo < 64 && hi >= 0 ? (~0ull << lo) & (hi < 63 ? (2ull << hi) - 1 : ~0ull) : 0ull;
@@ -337,11 +396,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
 #pragma unroll
         for (int u = 0; u < NV; ++u) v[u] = fmaf(slope[c], (float)tok(u), v[u]);
         if (p.parents && p0 + kS > base) {  // a node's position is its depth's, not its place's
+          const uint64_t ups = above(token[c]);
 #pragma unroll
           for (int u = 0; u < NV; ++u) {
             const int a = p0 + 16 * g + tok(u) - base;
             if (a > 0 && a < 64) {
-              const int d = __builtin_popcountll(above[c] & ((1ull << a) - 1));
+              const int d = __builtin_popcountll(ups & ((1ull << a) - 1));
               v[u] = fmaf(slope[c], (float)(d - a), v[u]);
             }
           }
@@ -371,14 +431,16 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       top = fmaxf(max_xor32(top) * p.scale, mx[c]);
       const float shrink = __builtin_amdgcn_exp2f(mx[c] - top);
       mx[c] = top;
-      const float sub = at * p.scale - top;
+      const float sub = at * p.scale - top + (VS ? 15.f : 0.f);  // (VS: P up to 2^15)
 #pragma unroll
       for (int u = 0; u < NV; ++u) v[u] = __builtin_amdgcn_exp2f(fmaf(v[u], p.scale, sub));
-      if (masked) {
-        const uint64_t mg = mask >> (16 * g);
+      if (bad != 0) {
+        float nan;
+        asm("v_mov_b32 %0, 0x7fc00000" : "=v"(nan));
+        const uint64_t bg = (bad & mask) >> (16 * g);
 #pragma unroll
         for (int u = 0; u < NV; ++u)
-          if (!(mg >> tok(u) & 1)) v[u] = 0.f;
+          if (bg >> tok(u) & 1) v[u] = nan;
       }
       float add = v[0], add2 = v[1];
 #pragma unroll
@@ -394,26 +456,23 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
 #pragma unroll
           for (int r = 0; r < NR; ++r) o[c][a][r] *= both;
       }
+      if constexpr (VS) {
 #pragma unroll
-      for (int u = 0; u < NV; u += 4) {
-        const f32x4 s4 = *reinterpret_cast<const f32x4*>(sc_lds + 64 + 16 * g + tok(u));
+        for (int u = 0; u < NV; ++u) pf[c][u / 8][0][u % 8] = (_Float16)v[u];
+      } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x = v[u + e] * s4[e];
-          if constexpr (PP == 2) asm("" : "+v"(x));  // (one rounding of x for both terms)
-          const int i = (u + e) / 8, m = (u + e) % 8;
-          const _Float16 hi = (_Float16)x;
-          pf[c][i][0][m] = hi;
-          if constexpr (PP == 2) pf[c][i][PP - 1][m] = (_Float16)(x - (float)hi);
+        for (int u = 0; u < NV; u += 4) {
+          const f32x4 s4 = *reinterpret_cast<const f32x4*>(sc_lds + 64 + 16 * g + tok(u));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = v[u + e] * s4[e];
+            if constexpr (PP == 2) asm("" : "+v"(x));  // (one rounding of x for both terms)
+            const int i = (u + e) / 8, m = (u + e) % 8;
+            const _Float16 hi = (_Float16)x;
+            pf[c][i][0][m] = hi;
+            if constexpr (PP == 2) pf[c][i][PP - 1][m] = (_Float16)(x - (float)hi);
+          }
         }
-      }
-      if (masked) {  // (a scale that is NaN stays with the rows that see it)
-        const uint64_t mg = mask >> (16 * g);
-#pragma unroll
-        for (int u = 0; u < NV; ++u)
-          if (!(mg >> tok(u) & 1))
-#pragma unroll
-            for (int e = 0; e < PP; ++e) pf[c][u / 8][e][u % 8] = (_Float16)0.f;
       }
     }
 
@@ -435,7 +494,13 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
         const u32x4 r = vr[a * NX + (i >> 1)];
-        const f16x8 f = to_f16<I8>(r[2 * (i & 1)], r[2 * (i & 1) + 1]);
+        f16x8 f;
+        if constexpr (VS)
+          f = to_f16_small(r[2 * (i & 1)], r[2 * (i & 1) + 1]) *
+              *reinterpret_cast<const f16x8*>(reinterpret_cast<const _Float16*>(sc_lds + 64) + 16 * g +
+                                              32 * (i >> 1) + 8 * (i & 1));
+        else
+          f = to_f16<I8>(r[2 * (i & 1)], r[2 * (i & 1) + 1]);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -445,7 +510,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   }
 
   // ---- output: value u of a lane is column 32 (u / 16) + 16 g + u % 16 (W = 32) or 16 g + u
-  const int back = octave == -1000 ? 0 : octave - 15;
+  const int back = octave == -1000 ? 0 : octave - 15 + (VS ? 9 - 15 : 0);
 #pragma unroll
   for (int c = 0; c < NC; ++c) {  // the groups' shares of the sums
     if constexpr (W == 16) {
@@ -453,7 +518,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       pair16(__float_as_uint(sum[c]), x, y);
       sum[c] = __uint_as_float(x) + __uint_as_float(y);
     }
-    sum[c] = sum_xor32(sum[c]);
+    sum[c] = sum_xor32(sum[c]) * (VS ? 0x1p-15f : 1.f);
   }
   T* const out0 = (T*)scalar_ptr(reinterpret_cast<T*>(p.out) + (row0 + m0) * kD);
   if (workers == 1) {
@@ -462,7 +527,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       const uint32_t m = c * W + col;
       if (m >= nrows) continue;
       const Joined j = finish(mx[c], sum[c], p.off_by_one);
-      const bool none = !live[c] || sum[c] == 0.f;
+      const bool none = token[c] >= n || sum[c] == 0.f;
       // (off by one: the row's own scale between its maximum and the denominator's)
       const float f = none ? 0.f : __builtin_amdgcn_exp2f(mx[c] - j.m) / j.l;
       T* dst = out0 + m * kD + 16 * g;
@@ -497,8 +562,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
                 __builtin_ldexpf(a[u % NR + 2], back), __builtin_ldexpf(a[u % NR + 3], back)};
     }
     if (g == 0) {
-      ml[2 * (wave * nrows + m)] = live[c] ? mx[c] : kLowest;
-      ml[2 * (wave * nrows + m) + 1] = live[c] ? sum[c] : 0.f;
+      ml[2 * (wave * nrows + m)] = token[c] < n ? mx[c] : kLowest;
+      ml[2 * (wave * nrows + m) + 1] = token[c] < n ? sum[c] : 0.f;
     }
   }
   __syncthreads();
@@ -518,8 +583,9 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     }
     if (p.splits > 1) {
       const int64_t at = (int64_t)it * QB + m;
-      *reinterpret_cast<f32x4*>(p.part + at * kD + 4 * x) = acc;
-      if (x == 0) *reinterpret_cast<f32x2*>(p.part_ml + at * 2) = f32x2{top, l};
+      put2(p.part + at * kD + 4 * x, acc[0], acc[1]);
+      put2(p.part + at * kD + 4 * x + 2, acc[2], acc[3]);
+      if (x == 0) put2(p.part_ml + at * 2, top, l);
     } else {
       const Joined j = finish(top, l, p.off_by_one);
       const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
@@ -528,9 +594,20 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
         p.lse[row0 + m0 + m] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
     }
   }
+  if (p.splits == 1 || !p.ticket) return;
+  // the last workgroup of the block to get here joins its parts
+  wait_tiles<0>();  // (this thread's part is where every XCD sees it)
+  __syncthreads();
+  uint32_t* const drawn = reinterpret_cast<uint32_t*>(smem);
+  if (tid == 0)
+    *drawn = (uint32_t)__hip_atomic_fetch_add(p.ticket + bb, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (*drawn != p.splits - 1) return;
+  if (tid == 0) __hip_atomic_store(p.ticket + bb, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw) join_rows<T, QB>(p, bb, e >> 4, e & 15, row0 + m0);
 }
 
-// Joins the parts of split row blocks: 16 threads per row.
+// The same in a launch of its own, where a window has no tickets for so many row blocks: 16 threads per row.
 template <typename T, int QB>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
   const uint32_t e = __builtin_amdgcn_workgroup_id_x() * 256 + __builtin_amdgcn_workitem_id_x();
@@ -546,26 +623,8 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
     at0 = blk * QB;
     nrows = min((uint32_t)QB, p.M - at0);
   }
-  if (m >= nrows) return;
-  float top = kLowest;
-  for (uint32_t s = 0; s < p.splits; ++s)
-    top = fmaxf(top, p.part_ml[(((int64_t)bb * p.splits + s) * QB + m) * 2]);
-  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (uint32_t s = 0; s < p.splits; ++s) {
-    const int64_t at = ((int64_t)bb * p.splits + s) * QB + m;
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + at * 2);
-    if (ml[1] == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml[0] - top);
-    l = fmaf(ml[1], f, l);
-    acc += *reinterpret_cast<const f32x4*>(p.part + at * kD + 4 * x) * f;
-  }
-  const Joined j = finish(top, l, p.off_by_one);
-  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
   const uint32_t b = bh / p.Hkv, h = bh - b * p.Hkv;
-  const int64_t r = (int64_t)(b * p.H + h * p.G) * p.T + at0 + m;
-  store4(reinterpret_cast<T*>(p.out) + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
-  if (p.lse && x == 0) p.lse[r] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+  if (m < nrows) join_rows<T, QB>(p, bb, m, x, (int64_t)(b * p.H + h * p.G) * p.T + at0);
 }
 
 }  // namespace
@@ -641,6 +700,8 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
   p.lse = lse;
   p.part = static_cast<float*>(ws);
   p.part_ml = p.part + (size_t)a.groups * a.splits * a.rows * kD;
+  // (a window has 2 H tickets per sequence)
+  p.ticket = a.blocks <= 2 * (int64_t)p.G ? w.ticket : nullptr;
   const float s = fabsf(w.attn_scale);
   p.scale = (s > 0.f ? s : 1.f) * kLog2e;
   p.unscale = s > 0.f ? 1.f / s : 1.f;
@@ -659,7 +720,7 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
     else if (a.rows == 32) launch_kernel(name, window_attn_kernel<T_, I8, 32, 1>, grid, block, lds, stream, p);
     else if constexpr (sizeof(T_) == 2)
       launch_kernel(name, window_attn_kernel<T_, I8, 32, 2>, grid, block, lds, stream, p);
-    if (a.splits > 1) {
+    if (a.splits > 1 && !p.ticket) {
       const dim3 joins((unsigned)((a.groups * a.rows * 16 + 255) / 256)), threads(256);
       name = "window_join_kernel";
       if (a.rows == 16) launch_kernel(name, window_join_kernel<T_, 16>, joins, threads, 0, stream, p);

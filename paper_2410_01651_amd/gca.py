@@ -865,11 +865,14 @@ def verify(p, tokens, u, q=None, parents=None, lengths=None, path=None, count=No
     xp = _cache_ptr(c, next, "next", i32, (B,))
     with _at(c, stream) as st:
         if path is None:
-            path, op = _new(c, bt, i32, tokens)
+            path = tokens.new_empty(bt)
+            op = path.data_ptr()
         if count is None:
-            count, cp = _new(c, (B,), i32)
+            count = tokens.new_empty(B)
+            cp = count.data_ptr()
         if next is None:
-            next, xp = _new(c, (B,), i32)
+            next = tokens.new_empty(B)
+            xp = next.data_ptr()
         if ws is None:
             ws = verify_workspace(B, T, V, c.device)[0]
         _check(lib().gca_verify(B, T, V, pp, qp, tp, rp, up, np_, op, cp, xp,

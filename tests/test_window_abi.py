@@ -148,10 +148,10 @@ def test_workspace(gca):
     assert _attn(gca, big, T=1, nbytes=need - 1) == gca.GCA_ERR_WORKSPACE
     assert _attn(gca, big, T=1, ws=None) == gca.GCA_ERR_WORKSPACE
     assert _attn(gca, big, T=1, ws=FAKE + 128) != gca.GCA_OK
-    need = L.gca_verify_workspace_size(2, 5, 1000)
+    need = L.gca_verify_workspace_size(2, 5, 200000)
     assert need > 0 and need % 256 == 0
-    assert _verify(gca, nbytes=need - 1) == gca.GCA_ERR_WORKSPACE
-    assert _verify(gca, ws=None) == gca.GCA_ERR_WORKSPACE
+    assert _verify(gca, V=200000, nbytes=need - 1) == gca.GCA_ERR_WORKSPACE
+    assert _verify(gca, V=200000, ws=None) == gca.GCA_ERR_WORKSPACE
 
 
 def test_a_refused_size_leaves_the_error_as_it_was(gca):
