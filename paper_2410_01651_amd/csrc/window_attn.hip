@@ -296,6 +296,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
   Acc o[NC][NA];
   float mx[NC], sum[NC];
   int octave = -1000;  // of u
+  float limit = 0.f;   // 2^octave
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     mx[c] = kLowest;
@@ -314,14 +315,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
     const int from = first - p0, to = length - p0;  // what may be seen of the tile
     const bool here = lane >= from && lane < to;
     const float nu = here ? vsc : 0.f;
-    const float big = max64(nu);
     int up_by = 0;  // octaves that u grows by
-    if (big > 0.f) {
-      const int e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(big));
-      if (e > octave) {
-        up_by = octave == -1000 ? 0 : e - octave;
-        octave = e;
-      }
+    if (__ballot(nu > limit) != 0) {
+      const int e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(max64(nu)));
+      up_by = octave == -1000 ? 0 : e - octave;
+      octave = e;
+      limit = __builtin_ldexpf(1.f, e);
     }
     wave_lds_order();
     sc_lds[lane] = ksc;
@@ -436,7 +435,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
       for (int u = 0; u < NV; ++u) v[u] = __builtin_amdgcn_exp2f(fmaf(v[u], p.scale, sub));
       if (bad != 0) {
         float nan;
-        asm("v_mov_b32 %0, 0x7fc00000" : "=v"(nan));
+        asm volatile("v_mov_b32 %0, 0x7fc00000" : "=v"(nan));
         const uint64_t bg = (bad & mask) >> (16 * g);
 #pragma unroll
         for (int u = 0; u < NV; ++u)
