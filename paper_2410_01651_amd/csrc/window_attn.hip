@@ -128,8 +128,8 @@ __device__ __forceinline__ void join_rows(const WindowParams& p, uint32_t bb, ui
 
 // (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
 // floating point flags and would be called.)
-// T: type of the queries; W: MFMA tile; NC: column blocks of W query rows.
-template <typename T, bool I8, int W, int NC>
+// T: type of the queries; W: MFMA tile; NC: column blocks of W query rows; TREE: the new tokens are a tree.
+template <typename T, bool I8, int W, int NC, bool TREE>
 __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) void window_attn_kernel(WindowParams p) {
   constexpr bool kB16 = sizeof(T) == 2;
   constexpr int NG = 64 / W;           // lane groups
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
 
   // ---- the tree: lane i holds node i's ancestors and itself as bits
   uint64_t up = 0;
-  if (p.parents) {
+  if constexpr (TREE) {
     const int i = lane;
     int par = p.parents[(int64_t)b * p.T + min((uint32_t)i, p.T - 1)];
     par = par >= 0 && par < i ? par : i;
@@ -196,9 +196,13 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
 
   // ---- this lane's rows
   uint32_t row[NC];    // of the group
-  int token[NC];
   int depth[NC];       // position - base
   float slope[NC];     // in units of a score before its scale
+  auto token = [&](int c) {  // (a node's is formed again where it is wanted, to have the registers)
+    if constexpr (!TREE) return depth[c];
+    const uint32_t m = m0 + min((uint32_t)opaque(c * W + col), nrows - 1);
+    return (int)(m - m / p.T * p.T);
+  };
   // a node's ancestors and itself
   auto above = [&](int i) {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * i, (int)(uint32_t)up);
@@ -210,22 +214,22 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
     const uint32_t m = m0 + min((uint32_t)(c * W + col), nrows - 1);
     const uint32_t gh = m / p.T, t = m - gh * p.T;
     row[c] = m;
-    token[c] = depth[c] = (int)t;
-    if (p.parents) depth[c] = __builtin_popcountll(above((int)t)) - 1;
+    depth[c] = (int)t;
+    if constexpr (TREE) depth[c] = __builtin_popcountll(above((int)t)) - 1;
     slope[c] = p.slopes ? p.slopes[h * p.G + gh] * p.unscale : 0.f;
   }
 
   // ---- tiles of 64 positions that the rows see: [t0, t1)
-  const int dmin = p.parents ? 0 : (int)tmin, dmax = p.parents ? kTreeNodes - 1 : (int)tmax;
+  const int dmin = TREE ? 0 : (int)tmin, dmax = TREE ? kTreeNodes - 1 : (int)tmax;
   const int first = p.window ? max(base + dmin - p.window + 1, 0) : 0;
-  const int last = p.parents ? length - 1 : min(base + (int)tmax, length - 1);  // position
+  const int last = TREE ? length - 1 : min(base + (int)tmax, length - 1);  // position
   const int t0 = first >> 6;
   int t1 = (last >> 6) + 1;
   if (!p.ring) t1 = min(t1, (int)p.ring_tiles);
   if ((int)tmin >= n) t1 = t0;
   // every row sees the whole of a tile within [full0, full1]
   const int full0 = p.window ? base + dmax - p.window + 1 : 0;
-  const int full1 = p.parents ? base - 1 : base + (int)tmin;
+  const int full1 = TREE ? base - 1 : base + (int)tmin;
   const uint32_t workers = p.splits * nw, me = split * nw + wave;
 
   const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
@@ -292,7 +296,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
     }
   }
 
-  float* const sc_lds = smem + wave * 128;  // this wave's scales: 64 of keys, 64 of values
+  float* const sc_lds = smem + wave * 192;  // this wave's scales: 64 of keys, 64 of values; what is NaN
   Acc o[NC][NA];
   float mx[NC], sum[NC];
   int octave = -1000;  // of u
@@ -352,9 +356,13 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
           for (int e = 0; e < QP; ++e) st[c][a] = mma(f, qf[c][i][e], st[c][a]);
       }
     }
-    load_tile(kr, p.k, sn, more);
-    ksc = load_scale(p.ks, sn, more);
-    vsc = load_scale(p.vs, sn, more);
+    // (the next keys: with two column blocks behind the first one's softmax, which leaves their registers)
+    auto next_keys = [&] {
+      load_tile(kr, p.k, sn, more);
+      ksc = load_scale(p.ks, sn, more);
+      vsc = load_scale(p.vs, sn, more);
+    };
+    if constexpr (NC == 1) next_keys();
 
     const bool masked = p0 < full0 || p0 + kS - 1 > full1;
     f16x8 pf[NC][NK][PP];
@@ -373,29 +381,40 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
           for (int e = 0; e < 4; ++e) v[u + e] *= s4[e];
         }
       }
-      uint64_t mask = ~0ull;
-      if (masked) {
+      // tokens of the tile that the row sees: first .. last of them in a chain, in a tree bits
+      const int lo = (p.window ? max(base + depth[c] - p.window + 1 - p0, 0) : 0) - 16 * g;
+      const int hi = min(base + depth[c] - p0, to - 1) - 16 * g;
+      uint64_t bits = ~0ull;
+      if (TREE && masked) {
         const int off = base - p0;  // the first new token
-        const int lo = p.window ? max(base + depth[c] - p.window + 1 - p0, 0) : 0;
-        if (p.parents) {
-          mask = off >= 64 ? ~0ull : off > 0 ? (1ull << off) - 1 : 0ull;
-          mask = lo < 64 ? mask & (~0ull << lo) : 0ull;
-          uint64_t sees = above(token[c]);
-          if (p.window)  // without ancestors `window` levels up or more
-            for (int x = depth[c] - p.window; x >= 0; --x) sees &= sees - 1;
-          if (off < 64) mask |= off >= 0 ? sees << off : off > -64 ? sees >> -off : 0ull;
-        } else {
-          const int hi = off + depth[c];  // the row's own
-          mask = lo < 64 && hi >= 0 ? (~0ull << lo) & (hi < 63 ? (2ull << hi) - 1 : ~0ull) : 0ull;
+        bits = off >= 64 ? ~0ull : off > 0 ? (1ull << off) - 1 : 0ull;
+        uint64_t sees = above(token(c));
+        if (p.window) {  // without ancestors `window` levels up or more
+          const int l = lo + 16 * g;
+          bits = l < 64 ? bits & (~0ull << l) : 0ull;
+          for (int x = depth[c] - p.window; x >= 0; --x) sees &= sees - 1;
         }
-        if (to < 64) mask &= to > 0 ? (1ull << to) - 1 : 0ull;
+        if (off < 64) bits |= off >= 0 ? sees << off : off > -64 ? sees >> -off : 0ull;
+        if (to < 64) bits &= to > 0 ? (1ull << to) - 1 : 0ull;
+        bits >>= 16 * g;
+      }
+      if (bad != 0) {  // NaN for the rows that see it (the others are masked behind)
+        wave_lds_order();
+        reinterpret_cast<uint32_t*>(sc_lds + 128)[lane] = bad >> lane & 1 ? 0x7fc00000u : 0u;
+        wave_lds_order();
+#pragma unroll
+        for (int u = 0; u < NV; u += 4) {
+          const f32x4 s4 = *reinterpret_cast<const f32x4*>(sc_lds + 128 + 16 * g + tok(u));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[u + e] += s4[e];
+        }
       }
       if (p.slopes) {
         // relative to the tile's first token; its own place joins the maximum below
 #pragma unroll
         for (int u = 0; u < NV; ++u) v[u] = fmaf(slope[c], (float)tok(u), v[u]);
-        if (p.parents && p0 + kS > base) {  // a node's position is its depth's, not its place's
-          const uint64_t ups = above(token[c]);
+        if (TREE && p0 + kS > base) {  // a node's position is its depth's, not its place's
+          const uint64_t ups = above(token(c));
 #pragma unroll
           for (int u = 0; u < NV; ++u) {
             const int a = p0 + 16 * g + tok(u) - base;
@@ -406,11 +425,25 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
           }
         }
       }
-      if (masked) {
-        const uint64_t mg = mask >> (16 * g);
+      if constexpr (TREE) {
+        if (masked) {
 #pragma unroll
-        for (int u = 0; u < NV; ++u)
-          if (!(mg >> tok(u) & 1)) v[u] = -INFINITY;
+          for (int u = 0; u < NV; ++u)
+            if (!(bits >> tok(u) & 1)) v[u] = -INFINITY;
+        }
+      } else {
+        if (p0 < full0) {
+          const int x = opaque(lo);
+#pragma unroll
+          for (int u = 0; u < NV; ++u)
+            if (tok(u) < x) v[u] = -INFINITY;
+        }
+        if (p0 + kS - 1 > full1) {
+          const int x = opaque(hi);
+#pragma unroll
+          for (int u = 0; u < NV; ++u)
+            if (tok(u) > x) v[u] = -INFINITY;
+        }
       }
       float top = fmaxf(fmaxf(v[0], v[1]), v[2]), top2 = fmaxf(fmaxf(v[3], v[4]), v[5]);
 #pragma unroll
@@ -433,14 +466,6 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
       const float sub = at * p.scale - top + (VS ? 15.f : 0.f);  // (VS: P up to 2^15)
 #pragma unroll
       for (int u = 0; u < NV; ++u) v[u] = __builtin_amdgcn_exp2f(fmaf(v[u], p.scale, sub));
-      if (bad != 0) {
-        float nan;
-        asm volatile("v_mov_b32 %0, 0x7fc00000" : "=v"(nan));
-        const uint64_t bg = (bad & mask) >> (16 * g);
-#pragma unroll
-        for (int u = 0; u < NV; ++u)
-          if (bg >> tok(u) & 1) v[u] = nan;
-      }
       float add = v[0], add2 = v[1];
 #pragma unroll
       for (int u = 2; u < NV; u += 2) {
@@ -473,6 +498,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
           }
         }
       }
+      if (NC > 1 && c == 0) next_keys();
     }
 
     // O^T += M^T P^T (numbers behind the newest token are cleared: they may be anything)
@@ -526,7 +552,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
       const uint32_t m = c * W + col;
       if (m >= nrows) continue;
       const Joined j = finish(mx[c], sum[c], p.off_by_one);
-      const bool none = token[c] >= n || sum[c] == 0.f;
+      const bool none = token(c) >= n || sum[c] == 0.f;
       // (off by one: the row's own scale between its maximum and the denominator's)
       const float f = none ? 0.f : __builtin_amdgcn_exp2f(mx[c] - j.m) / j.l;
       T* dst = out0 + m * kD + 16 * g;
@@ -561,8 +587,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
                 __builtin_ldexpf(a[u % NR + 2], back), __builtin_ldexpf(a[u % NR + 3], back)};
     }
     if (g == 0) {
-      ml[2 * (wave * nrows + m)] = token[c] < n ? mx[c] : kLowest;
-      ml[2 * (wave * nrows + m) + 1] = token[c] < n ? sum[c] : 0.f;
+      ml[2 * (wave * nrows + m)] = token(c) < n ? mx[c] : kLowest;
+      ml[2 * (wave * nrows + m) + 1] = token(c) < n ? sum[c] : 0.f;
     }
   }
   __syncthreads();
@@ -707,7 +733,7 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
   p.negate = w.attn_scale < 0.f ? (w.dtype == GCA_BF16 ? 0x80008000u : 0x80000000u) : 0u;
   p.keep = s > 0.f ? 0xffffffffu : 0u;
   p.off_by_one = w.off_by_one;
-  size_t lds = (size_t)a.waves * 128 * sizeof(float);
+  size_t lds = (size_t)a.waves * 192 * sizeof(float);
   const size_t parts = a.waves * a.splits > 1 ? (size_t)a.waves * a.rows * (kD + 2) * sizeof(float) : 0;
   if (parts > lds) lds = parts;
   const dim3 grid((p.items + 7) / 8 * 8), block(64 * a.waves);
@@ -715,10 +741,14 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
     using T_ = decltype(tag);
     constexpr bool I8 = decltype(i8)::value;
     const char* name = "window_attn_kernel";
-    if (a.rows == 16) launch_kernel(name, window_attn_kernel<T_, I8, 16, 1>, grid, block, lds, stream, p);
-    else if (a.rows == 32) launch_kernel(name, window_attn_kernel<T_, I8, 32, 1>, grid, block, lds, stream, p);
-    else if constexpr (sizeof(T_) == 2)
-      launch_kernel(name, window_attn_kernel<T_, I8, 32, 2>, grid, block, lds, stream, p);
+    auto attend = [&](auto tree) {
+      constexpr bool TREE = decltype(tree)::value;
+      if (a.rows == 16) launch_kernel(name, window_attn_kernel<T_, I8, 16, 1, TREE>, grid, block, lds, stream, p);
+      else if (a.rows == 32) launch_kernel(name, window_attn_kernel<T_, I8, 32, 1, TREE>, grid, block, lds, stream, p);
+      else if constexpr (sizeof(T_) == 2)
+        launch_kernel(name, window_attn_kernel<T_, I8, 32, 2, TREE>, grid, block, lds, stream, p);
+    };
+    parents ? attend(std::true_type{}) : attend(std::false_type{});
     if (a.splits > 1 && !p.ticket) {
       const dim3 joins((unsigned)((a.groups * a.rows * 16 + 255) / 256)), threads(256);
       name = "window_join_kernel";
