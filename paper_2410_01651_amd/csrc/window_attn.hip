@@ -130,7 +130,7 @@ __device__ __forceinline__ void join_rows(const WindowParams& p, uint32_t bb, ui
 // floating point flags and would be called.)
 // T: type of the queries; W: MFMA tile; NC: column blocks of W query rows; TREE: the new tokens are a tree.
 template <typename T, bool I8, int W, int NC, bool TREE>
-__global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) void window_attn_kernel(WindowParams p) {
+__global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowParams p) {
   constexpr bool kB16 = sizeof(T) == 2;
   constexpr int NG = 64 / W;           // lane groups
   constexpr int NA = 64 / W;           // blocks of W tokens (or columns) per tile
@@ -143,7 +143,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
   constexpr int QB = W * NC;           // query rows per item
   // Values take their scales along (e4m3: powers of two, so exactly) where two column blocks share them; else
   // the probabilities do, which are then fewer.
-  constexpr bool VS = !I8 && kB16 && NC == 2;
+  constexpr bool VS = NC == 2;
+  static_assert(NC == 1 || (kB16 && !I8), "64 rows: e4m3 numbers, bf16 tensors");
   typedef __attribute__((ext_vector_type(NR))) float Acc;
   extern __shared__ __attribute__((aligned(16))) float smem[];
 
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, W == 16 && sizeof(T) == 2 ? 4 : 2) 
     sum[c] = sum_xor32(sum[c]) * (VS ? 0x1p-15f : 1.f);
   }
   T* const out0 = (T*)scalar_ptr(reinterpret_cast<T*>(p.out) + (row0 + m0) * kD);
-  if (workers == 1) {
+  if (NC == 2 || workers == 1) {  // (64 rows: always a wave each)
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const uint32_t m = c * W + col;
@@ -656,10 +657,13 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
 
 namespace {
 constexpr int kWavesPerCu = 8;
-int most_waves(int rows) { return rows == 64 ? 4 : kMaxWaves; }  // (64 KiB of LDS for the parts)
+// 64 rows unpack a tile for twice the rows, but leave two waves per SIMD: where such blocks, a wave each, fill
+// the chip.
 int rows_of(const gca_window& w, int64_t T) {
-  const int64_t M = w.H / w.Hkv * T;
-  return M <= 16 ? 16 : M <= 32 || w.dtype != GCA_BF16 ? 32 : 64;
+  const int64_t G = w.H / w.Hkv, M = G * T, blocks = T >= 64 ? G * ((T + 63) / 64) : (M + 63) / 64;
+  if (M <= 16) return 16;
+  const bool can = w.dtype == GCA_BF16 && w.format == GCA_E4M3;
+  return can && (int64_t)w.B * w.Hkv * blocks >= kWavesPerCu * device_cus() ? 64 : 32;
 }
 // Tiles that a row block may see.
 int64_t tiles_seen(const gca_window& w, int64_t T, int rows) {
@@ -675,24 +679,24 @@ WindowAttnPlan window_attn_plan(const gca_window& w, int64_t T) {
   a.per_head = T >= a.rows ? (T + a.rows - 1) / a.rows : 0;
   a.blocks = a.per_head ? G * a.per_head : (M + a.rows - 1) / a.rows;
   a.groups = (int64_t)w.B * w.Hkv * a.blocks;
-  const int64_t tiles = tiles_seen(w, T, a.rows), most = most_waves(a.rows), fill = kWavesPerCu * device_cus();
+  const int64_t tiles = tiles_seen(w, T, a.rows), fill = kWavesPerCu * device_cus();
   a.waves = 1;
-  while (a.waves < most && 2 * a.waves <= tiles && a.groups * a.waves < fill) a.waves *= 2;
+  while (a.waves < kMaxWaves && 2 * a.waves <= tiles && a.groups * a.waves < fill) a.waves *= 2;
   // more workgroups where that leaves each wave two tiles at least
   int64_t splits = 1;
-  if (a.waves == most) {
-    splits = fill / (a.groups * most);
-    if (splits > tiles / (2 * most)) splits = tiles / (2 * most);
+  if (a.waves == kMaxWaves) {
+    splits = fill / (a.groups * kMaxWaves);
+    if (splits > tiles / (2 * kMaxWaves)) splits = tiles / (2 * kMaxWaves);
   }
   a.splits = (int)(splits < 1 ? 1 : splits);
   return a;
 }
 
 size_t window_workspace(const gca_window& w, int64_t T) {
-  // (what any number of row blocks of this height asks for: it then never falls as T grows)
-  const int rows = rows_of(w, T), most = most_waves(rows);
-  if (tiles_seen(w, T, rows) < 4 * most) return 0;
-  return align256((size_t)(kWavesPerCu * device_cus() / most) * rows * (kD + 2) * sizeof(float));
+  // (what any number of row blocks of this height, or of 32, asks for: it then never falls as T grows)
+  const int rows = rows_of(w, T) == 16 ? 16 : 32;
+  if (tiles_seen(w, T, rows) < 4 * kMaxWaves) return 0;
+  return align256((size_t)(kWavesPerCu * device_cus() / kMaxWaves) * rows * (kD + 2) * sizeof(float));
 }
 
 hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t* parents, const int32_t* lengths,
@@ -745,7 +749,7 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
       constexpr bool TREE = decltype(tree)::value;
       if (a.rows == 16) launch_kernel(name, window_attn_kernel<T_, I8, 16, 1, TREE>, grid, block, lds, stream, p);
       else if (a.rows == 32) launch_kernel(name, window_attn_kernel<T_, I8, 32, 1, TREE>, grid, block, lds, stream, p);
-      else if constexpr (sizeof(T_) == 2)
+      else if constexpr (sizeof(T_) == 2 && !I8)
         launch_kernel(name, window_attn_kernel<T_, I8, 32, 2, TREE>, grid, block, lds, stream, p);
     };
     parents ? attend(std::true_type{}) : attend(std::false_type{});
@@ -753,8 +757,7 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
       const dim3 joins((unsigned)((a.groups * a.rows * 16 + 255) / 256)), threads(256);
       name = "window_join_kernel";
       if (a.rows == 16) launch_kernel(name, window_join_kernel<T_, 16>, joins, threads, 0, stream, p);
-      else if (a.rows == 32) launch_kernel(name, window_join_kernel<T_, 32>, joins, threads, 0, stream, p);
-      else if constexpr (sizeof(T_) == 2) launch_kernel(name, window_join_kernel<T_, 64>, joins, threads, 0, stream, p);
+      else launch_kernel(name, window_join_kernel<T_, 32>, joins, threads, 0, stream, p);
     }
   };
   if (w.dtype == GCA_BF16) w.format == GCA_INT8 ? run(__bf16{}, std::true_type{}) : run(__bf16{}, std::false_type{});
