@@ -37,7 +37,8 @@ struct WindowParams {
   uint32_t nw;              // waves per workgroup
   uint32_t Hkv, G, T, M;    // M = G T: query rows of a group
   uint32_t per_head;        // row blocks per head; 0: the group's rows are one list
-  uint32_t H;
+  uint32_t H, B;
+  uint32_t balance;         // workgroups go by the sequences' lengths
   uint32_t ring_tiles;      // capacity / 64
   int32_t ring, window;
   const int32_t* length;
@@ -59,6 +60,10 @@ struct WindowParams {
   uint32_t negate, keep;  // xor and and masks of one query entry (fp32) or two: the scale's sign, and zero
   int off_by_one;
 };
+
+// (By its bits, and where the compiler does not know them for a float's: to this file's comparisons of floats
+// NaN may be anything.)
+__device__ __forceinline__ bool is_zero(float x) { return opaque((int)__float_as_uint(x)) << 1 == 0; }
 
 // out = sum_w exp2(m_w - m) o_w / (sum_w exp2(m_w - m) l_w), and the row's log-sum-exp.
 struct Joined {
@@ -84,16 +89,17 @@ __device__ __forceinline__ f32x2 get2(const float* at) {
   return f32x2{__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))};
 }
 
-// Joins the parts of a split row block: columns 4 x .. of its row m, row r0 + m of the output.
+// Joins parts first .. first + n - 1 of a row block: columns 4 x .. of its row m, row r0 + m of the output.
 template <typename T, int QB, uint32_t kAhead>  // kAhead: parts asked for at a time
-__device__ __forceinline__ void join_rows_by(const WindowParams& p, uint32_t bb, uint32_t m, uint32_t x, int64_t r0) {
+__device__ __forceinline__ void join_rows_by(const WindowParams& p, uint32_t first, uint32_t n, uint32_t m, uint32_t x,
+                                             int64_t r0) {
   float top = kLowest, l = 0.f;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (uint32_t s0 = 0; s0 < p.splits; s0 += kAhead) {
+  for (uint32_t s0 = 0; s0 < n; s0 += kAhead) {
     f32x2 ml[kAhead], a[kAhead], c[kAhead];
 #pragma unroll
     for (uint32_t s = 0; s < kAhead; ++s) {
-      const int64_t at = ((int64_t)bb * p.splits + min(s0 + s, p.splits - 1)) * QB + m;
+      const int64_t at = ((int64_t)first + min(s0 + s, n - 1)) * QB + m;
       ml[s] = get2(p.part_ml + at * 2);
       a[s] = get2(p.part + at * kD + 4 * x);
       c[s] = get2(p.part + at * kD + 4 * x + 2);
@@ -107,23 +113,24 @@ __device__ __forceinline__ void join_rows_by(const WindowParams& p, uint32_t bb,
     top = now;
 #pragma unroll
     for (uint32_t s = 0; s < kAhead; ++s) {
-      if (s0 + s >= p.splits || ml[s][1] == 0.f) continue;
+      if (s0 + s >= n || is_zero(ml[s][1])) continue;
       const float f = __builtin_amdgcn_exp2f(ml[s][0] - top);
       l = fmaf(ml[s][1], f, l);
       acc += f32x4{a[s][0], a[s][1], c[s][0], c[s][1]} * f;
     }
   }
   const Joined j = finish(top, l, p.off_by_one);
-  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
+  const float f = is_zero(l) ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
   const int64_t r = r0 + m;
   store4(reinterpret_cast<T*>(p.out) + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
-  if (p.lse && x == 0) p.lse[r] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+  if (p.lse && x == 0) p.lse[r] = is_zero(l) ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
 }
 
 template <typename T, int QB>
-__device__ __forceinline__ void join_rows(const WindowParams& p, uint32_t bb, uint32_t m, uint32_t x, int64_t r0) {
-  if (p.splits <= 4) join_rows_by<T, QB, 2>(p, bb, m, x, r0);
-  else join_rows_by<T, QB, 8>(p, bb, m, x, r0);
+__device__ __forceinline__ void join_rows(const WindowParams& p, uint32_t first, uint32_t n, uint32_t m, uint32_t x,
+                                          int64_t r0) {
+  if (n <= 4) join_rows_by<T, QB, 2>(p, first, n, m, x, r0);
+  else join_rows_by<T, QB, 8>(p, first, n, m, x, r0);
 }
 
 // (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
@@ -148,16 +155,71 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   typedef __attribute__((ext_vector_type(NR))) float Acc;
   extern __shared__ __attribute__((aligned(16))) float smem[];
 
-  const uint32_t it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
-  if (it >= p.items) return;
   const uint32_t tid = __builtin_amdgcn_workitem_id_x(), nw = p.nw;
   const int lane = tid & 63, g = lane / W, col = lane % W;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
-  // item = ((b Hkv + h) blocks + block) splits + split
-  const uint32_t bb = scalar(it / p.splits), split = it - bb * p.splits;
-  const uint32_t bh = scalar(bb / p.blocks), blk = bb - bh * p.blocks;
-  const uint32_t b = scalar(bh / p.Hkv), h = bh - b * p.Hkv;
+  // item = ((b Hkv + h) blocks + block) splits + split, unless the sequences' lengths have a say
+  uint32_t b, h, blk, split, splits = p.splits, it;
+  if (p.balance) {
+    // lane i: tiles of sequence i
+    const int len = p.length[min((uint32_t)lane, p.B - 1)];
+    const uint32_t tiles = min(((uint32_t)max(len, 1) + kS - 1) / kS, p.ring_tiles);
+    if (splits > 1) {
+      // B splits workgroups for each head and block, dealt out by tiles: one to each sequence, the
+      // others in proportion
+      it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
+      if (it >= p.items) return;
+      const uint32_t all = p.B * splits, hb = scalar(it / all), j = it - hb * all;
+      h = scalar(hb / p.blocks);
+      blk = hb - h * p.blocks;
+      uint32_t upto = (uint32_t)lane < p.B ? tiles : 0;
+#pragma unroll
+      for (int s = 1; s < 64; s *= 2) {
+        const uint32_t y = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane - s), (int)upto);
+        upto += lane >= s ? y : 0;
+      }
+      const uint32_t others = all - p.B, before = upto - ((uint32_t)lane < p.B ? tiles : 0);
+      const float each = (float)others / (float)__builtin_amdgcn_readlane((int)upto, 63);
+      const uint32_t from = lane + min((uint32_t)((float)before * each), others);
+      const uint32_t to = lane + 1 + min((uint32_t)((float)upto * each), others);
+      b = __builtin_popcountll(__ballot((uint32_t)lane < p.B && from <= j)) - 1;
+      split = j - (uint32_t)__builtin_amdgcn_readlane((int)from, (int)b);
+      splits = (uint32_t)__builtin_amdgcn_readlane((int)to, (int)b) - (j - split);
+      if (split >= splits) return;
+    } else {
+      // (sequence, head) pairs from the longest on are dealt to the XCDs there and back, and the second half of each
+      // XCD's comes in reverse, so that workgroups that share a CU make up for one another
+      const uint32_t pairs = p.B * p.Hkv, rounds = (pairs + 7) / 8;
+      const uint32_t bid = __builtin_amdgcn_workgroup_id_x(), xcd = bid & 7;
+      uint32_t i = scalar((bid >> 3) / p.blocks);
+      blk = (bid >> 3) - i * p.blocks;
+      const uint32_t half = (rounds + 1) / 2;
+      i = i < half ? i : rounds - 1 - (i - half);
+      const uint32_t pair = i * 8 + (i & 1 ? 7 - xcd : xcd);
+      if (pair >= pairs) return;
+      const uint32_t place = scalar(pair / p.Hkv);
+      h = pair - place * p.Hkv;
+      uint32_t rank = 0;  // of sequence `lane`
+      for (uint32_t x = 0; x < p.B; ++x) {
+        const uint32_t y = (uint32_t)__builtin_amdgcn_readlane((int)tiles, (int)x);
+        rank += y > tiles || (y == tiles && x < (uint32_t)lane) ? 1 : 0;
+      }
+      b = __builtin_ctzll(__ballot((uint32_t)lane < p.B && rank == place));
+      split = 0;
+      it = 0;
+    }
+  } else {
+    it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
+    if (it >= p.items) return;
+    const uint32_t at = scalar(it / splits);
+    split = it - at * splits;
+    const uint32_t bhs = scalar(at / p.blocks);
+    blk = at - bhs * p.blocks;
+    b = scalar(bhs / p.Hkv);
+    h = bhs - b * p.Hkv;
+  }
+  const uint32_t bh = b * p.Hkv + h, bb = bh * p.blocks + blk;
 
   // ---- the block's rows [m0, m0 + nrows) of the group's M, and the new tokens they belong to
   uint32_t m0, nrows, tmin, tmax;
@@ -231,7 +293,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   // every row sees the whole of a tile within [full0, full1]
   const int full0 = p.window ? base + dmax - p.window + 1 : 0;
   const int full1 = TREE ? base - 1 : base + (int)tmin;
-  const uint32_t workers = p.splits * nw, me = split * nw + wave;
+  const uint32_t workers = splits * nw, me = split * nw + wave;
 
   const uint32_t lane_row = W == 32 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3)
                                     : 16 * (col >> 2) + (col & 3);
@@ -553,7 +615,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       const uint32_t m = c * W + col;
       if (m >= nrows) continue;
       const Joined j = finish(mx[c], sum[c], p.off_by_one);
-      const bool none = token(c) >= n || sum[c] == 0.f;
+      const bool none = token(c) >= n || is_zero(sum[c]);
       // (off by one: the row's own scale between its maximum and the denominator's)
       const float f = none ? 0.f : __builtin_amdgcn_exp2f(mx[c] - j.m) / j.l;
       T* dst = out0 + m * kD + 16 * g;
@@ -601,26 +663,26 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     float l = 0.f;
     for (uint32_t y = 0; y < nw; ++y) {
       const float ly = ml[2 * (y * nrows + m) + 1];
-      if (ly == 0.f) continue;
+      if (is_zero(ly)) continue;
       const float f = __builtin_amdgcn_exp2f(ml[2 * (y * nrows + m)] - top);
       l = fmaf(ly, f, l);
       const f32x4 oy = *reinterpret_cast<const f32x4*>(part + (y * nrows + m) * kD + 4 * (x ^ (m & 15)));
       acc += oy * f;
     }
-    if (p.splits > 1) {
+    if (splits > 1) {
       const int64_t at = (int64_t)it * QB + m;
       put2(p.part + at * kD + 4 * x, acc[0], acc[1]);
       put2(p.part + at * kD + 4 * x + 2, acc[2], acc[3]);
       if (x == 0) put2(p.part_ml + at * 2, top, l);
     } else {
       const Joined j = finish(top, l, p.off_by_one);
-      const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
+      const float f = is_zero(l) ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
       store4(out0 + m * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
       if (p.lse && x == 0)
-        p.lse[row0 + m0 + m] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+        p.lse[row0 + m0 + m] = is_zero(l) ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
     }
   }
-  if (p.splits == 1 || !p.ticket) return;
+  if (splits == 1 || !p.ticket) return;
   // the last workgroup of the block to get here joins its parts
   wait_tiles<0>();  // (this thread's part is where every XCD sees it)
   __syncthreads();
@@ -628,9 +690,9 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   if (tid == 0)
     *drawn = (uint32_t)__hip_atomic_fetch_add(p.ticket + bb, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-  if (*drawn != p.splits - 1) return;
+  if (*drawn != splits - 1) return;
   if (tid == 0) __hip_atomic_store(p.ticket + bb, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw) join_rows<T, QB>(p, bb, e >> 4, e & 15, row0 + m0);
+  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw) join_rows<T, QB>(p, it - split, splits, e >> 4, e & 15, row0 + m0);
 }
 
 // The same in a launch of its own, where a window has no tickets for so many row blocks: 16 threads per row.
@@ -650,7 +712,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
     nrows = min((uint32_t)QB, p.M - at0);
   }
   const uint32_t b = bh / p.Hkv, h = bh - b * p.Hkv;
-  if (m < nrows) join_rows<T, QB>(p, bb, m, x, (int64_t)(b * p.H + h * p.G) * p.T + at0);
+  if (m < nrows) join_rows<T, QB>(p, bb * p.splits, p.splits, m, x, (int64_t)(b * p.H + h * p.G) * p.T + at0);
 }
 
 }  // namespace
@@ -709,6 +771,7 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
   p.nw = (uint32_t)a.waves;
   p.Hkv = w.Hkv;
   p.H = w.H;
+  p.B = w.B;
   p.G = w.H / w.Hkv;
   p.T = (uint32_t)T;
   p.M = (uint32_t)(p.G * T);
@@ -737,10 +800,14 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
   p.negate = w.attn_scale < 0.f ? (w.dtype == GCA_BF16 ? 0x80008000u : 0x80000000u) : 0u;
   p.keep = s > 0.f ? 0xffffffffu : 0u;
   p.off_by_one = w.off_by_one;
+  // Where every row sees its sequence's all, some may have far more to do.
+  p.balance = w.window == 0 && w.B > 1 && w.B <= 64 && w.capacity >= 1024 && (a.splits == 1 || p.ticket);
   size_t lds = (size_t)a.waves * 192 * sizeof(float);
   const size_t parts = a.waves * a.splits > 1 ? (size_t)a.waves * a.rows * (kD + 2) * sizeof(float) : 0;
   if (parts > lds) lds = parts;
-  const dim3 grid((p.items + 7) / 8 * 8), block(64 * a.waves);
+  const int64_t pairs = (int64_t)w.B * w.Hkv;  // (balanced without splits: whole rounds of the XCDs)
+  const dim3 grid((unsigned)(p.balance && a.splits == 1 ? (pairs + 7) / 8 * 8 * a.blocks : (p.items + 7) / 8 * 8));
+  const dim3 block(64 * a.waves);
   auto run = [&](auto tag, auto i8) {
     using T_ = decltype(tag);
     constexpr bool I8 = decltype(i8)::value;
