@@ -89,10 +89,10 @@ __device__ __forceinline__ f32x2 get2(const float* at) {
   return f32x2{__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))};
 }
 
-// Joins parts first .. first + n - 1 of a row block: columns 4 x .. of its row m, row r0 + m of the output.
+// Joins parts first .. first + n - 1 of a row block: columns 4 x .. of its row m, row r of the output.
 template <typename T, int QB, uint32_t kAhead>  // kAhead: parts asked for at a time
 __device__ __forceinline__ void join_rows_by(const WindowParams& p, uint32_t first, uint32_t n, uint32_t m, uint32_t x,
-                                             int64_t r0) {
+                                             int64_t r) {
   float top = kLowest, l = 0.f;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
   for (uint32_t s0 = 0; s0 < n; s0 += kAhead) {
@@ -121,16 +121,15 @@ __device__ __forceinline__ void join_rows_by(const WindowParams& p, uint32_t fir
   }
   const Joined j = finish(top, l, p.off_by_one);
   const float f = is_zero(l) ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
-  const int64_t r = r0 + m;
   store4(reinterpret_cast<T*>(p.out) + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
   if (p.lse && x == 0) p.lse[r] = is_zero(l) ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
 }
 
 template <typename T, int QB>
 __device__ __forceinline__ void join_rows(const WindowParams& p, uint32_t first, uint32_t n, uint32_t m, uint32_t x,
-                                          int64_t r0) {
-  if (n <= 4) join_rows_by<T, QB, 2>(p, first, n, m, x, r0);
-  else join_rows_by<T, QB, 8>(p, first, n, m, x, r0);
+                                          int64_t r) {
+  if (n <= 4) join_rows_by<T, QB, 2>(p, first, n, m, x, r);
+  else join_rows_by<T, QB, 8>(p, first, n, m, x, r);
 }
 
 // (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
@@ -221,7 +220,14 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   }
   const uint32_t bh = b * p.Hkv + h, bb = bh * p.blocks + blk;
 
-  // ---- the block's rows [m0, m0 + nrows) of the group's M, and the new tokens they belong to
+  const int length = max((int)scalar((uint32_t)p.length[b]), 0);
+  int n = p.lengths ? (int)scalar((uint32_t)p.lengths[b]) : (int)p.T;
+  n = max(min(n, (int)p.T), 0);
+  const int base = length - n;  // (negative only if fewer tokens were appended than `lengths` says)
+
+  // ---- the block's rows [m0, m0 + nrows), and the new tokens [tmin, tmax] they belong to.  Rows are cut
+  // head by head, or, short of a block per head, a group's rows with tokens as one list and those without behind it.
+  const uint32_t live = p.G * (uint32_t)n;
   uint32_t m0, nrows, tmin, tmax;
   if (p.per_head) {
     const uint32_t gh = scalar(blk / p.per_head);
@@ -232,14 +238,23 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   } else {
     m0 = blk * QB;
     nrows = min((uint32_t)QB, p.M - m0);
-    const uint32_t f = scalar(m0 / p.T), l = scalar((m0 + nrows - 1) / p.T);
-    tmin = f == l ? m0 - f * p.T : 0;
-    tmax = f == l ? tmin + nrows - 1 : p.T - 1;
+    tmin = (uint32_t)n;
+    tmax = p.T - 1;
+    if (m0 < live) {
+      const uint32_t end = min(m0 + nrows, live) - 1, f = scalar(m0 / (uint32_t)n), l = scalar(end / (uint32_t)n);
+      tmin = f == l ? m0 - f * n : 0;
+      tmax = f == l ? end - f * n : n - 1;
+    }
   }
-  const int length = max((int)scalar((uint32_t)p.length[b]), 0);
-  int n = p.lengths ? (int)scalar((uint32_t)p.lengths[b]) : (int)p.T;
-  n = max(min(n, (int)p.T), 0);
-  const int base = length - n;  // (negative only if fewer tokens were appended than `lengths` says)
+  // head of the group and token of row m of the block
+  auto place = [&](uint32_t m, uint32_t& gh, uint32_t& t) {
+    m += m0;
+    const bool behind = !p.per_head && m >= live;
+    const uint32_t per = p.per_head ? p.T : behind ? p.T - (uint32_t)n : (uint32_t)n;
+    m -= behind ? live : 0u;
+    gh = m / per;
+    t = m - gh * per + (behind ? (uint32_t)n : 0u);
+  };
 
   // ---- the tree: lane i holds node i's ancestors and itself as bits
   uint64_t up = 0;
@@ -263,8 +278,9 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   float slope[NC];     // in units of a score before its scale
   auto token = [&](int c) {  // (a node's is formed again where it is wanted, to have the registers)
     if constexpr (!TREE) return depth[c];
-    const uint32_t m = m0 + min((uint32_t)opaque(c * W + col), nrows - 1);
-    return (int)(m - m / p.T * p.T);
+    uint32_t gh, t;
+    place(min((uint32_t)opaque(c * W + col), nrows - 1), gh, t);
+    return (int)t;
   };
   // a node's ancestors and itself
   auto above = [&](int i) {
@@ -274,9 +290,9 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   };
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const uint32_t m = m0 + min((uint32_t)(c * W + col), nrows - 1);
-    const uint32_t gh = m / p.T, t = m - gh * p.T;
-    row[c] = m;
+    uint32_t gh, t;
+    place(min((uint32_t)(c * W + col), nrows - 1), gh, t);
+    row[c] = gh * p.T + t;
     depth[c] = (int)t;
     if constexpr (TREE) depth[c] = __builtin_popcountll(above((int)t)) - 1;
     slope[c] = p.slopes ? p.slopes[h * p.G + gh] * p.unscale : 0.f;
@@ -608,7 +624,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     }
     sum[c] = sum_xor32(sum[c]) * (VS ? 0x1p-15f : 1.f);
   }
-  T* const out0 = (T*)scalar_ptr(reinterpret_cast<T*>(p.out) + (row0 + m0) * kD);
+  T* const out0 = (T*)scalar_ptr(reinterpret_cast<T*>(p.out) + row0 * kD);
+  auto row_of = [&](uint32_t m) {  // row m of the block, among the group's
+    uint32_t gh, t;
+    place(m, gh, t);
+    return (int64_t)(gh * p.T + t);
+  };
   if (NC == 2 || workers == 1) {  // (64 rows: always a wave each)
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -618,7 +639,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       const bool none = token(c) >= n || is_zero(sum[c]);
       // (off by one: the row's own scale between its maximum and the denominator's)
       const float f = none ? 0.f : __builtin_amdgcn_exp2f(mx[c] - j.m) / j.l;
-      T* dst = out0 + m * kD + 16 * g;
+      const int64_t r = row_of(m);
+      T* dst = out0 + r * kD + 16 * g;
 #pragma unroll
       for (int u = 0; u < NV; u += 8) {
         float x[8];
@@ -628,7 +650,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
         store8(dst + (u / 16) * 32 + u % 16, x);
       }
       if (p.lse && g == 0)
-        p.lse[row0 + m0 + m] = none ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+        p.lse[row0 + r] = none ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
     }
     return;
   }
@@ -677,9 +699,10 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     } else {
       const Joined j = finish(top, l, p.off_by_one);
       const float f = is_zero(l) ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
-      store4(out0 + m * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
+      const int64_t r = row_of(m);
+      store4(out0 + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
       if (p.lse && x == 0)
-        p.lse[row0 + m0 + m] = is_zero(l) ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+        p.lse[row0 + r] = is_zero(l) ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
     }
   }
   if (splits == 1 || !p.ticket) return;
@@ -692,10 +715,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   __syncthreads();
   if (*drawn != splits - 1) return;
   if (tid == 0) __hip_atomic_store(p.ticket + bb, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw) join_rows<T, QB>(p, it - split, splits, e >> 4, e & 15, row0 + m0);
+  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw) 
+    join_rows<T, QB>(p, it - split, splits, e >> 4, e & 15, row0 + row_of(e >> 4));
 }
 
-// The same in a launch of its own, where a window has no tickets for so many row blocks: 16 threads per row.
+// The same in a launch of its own, where a window has no tickets for so many row blocks (cut head by head, then): 16
+// threads per row.
 template <typename T, int QB>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
   const uint32_t e = __builtin_amdgcn_workgroup_id_x() * 256 + __builtin_amdgcn_workitem_id_x();
@@ -712,7 +737,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
     nrows = min((uint32_t)QB, p.M - at0);
   }
   const uint32_t b = bh / p.Hkv, h = bh - b * p.Hkv;
-  if (m < nrows) join_rows<T, QB>(p, bb * p.splits, p.splits, m, x, (int64_t)(b * p.H + h * p.G) * p.T + at0);
+  if (m < nrows) join_rows<T, QB>(p, bb * p.splits, p.splits, m, x, (int64_t)(b * p.H + h * p.G) * p.T + at0 + m);
 }
 
 }  // namespace
