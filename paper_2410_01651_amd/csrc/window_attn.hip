@@ -160,54 +160,46 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
   // item = ((b Hkv + h) blocks + block) splits + split, unless the sequences' lengths have a say
   uint32_t b, h, blk, split, splits = p.splits, it;
+  uint32_t bare = 0;  // blocks from here on (of each head, cut head by head) that have no tokens, 0: none to be written here
   if (p.balance) {
-    // lane i: tiles of sequence i
-    const int len = p.length[min((uint32_t)lane, p.B - 1)];
-    const uint32_t tiles = min(((uint32_t)max(len, 1) + kS - 1) / kS, p.ring_tiles);
-    if (splits > 1) {
-      // B splits workgroups for each head and block, dealt out by tiles: one to each sequence, the
-      // others in proportion
-      it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
-      if (it >= p.items) return;
-      const uint32_t all = p.B * splits, hb = scalar(it / all), j = it - hb * all;
-      h = scalar(hb / p.blocks);
-      blk = hb - h * p.blocks;
-      uint32_t upto = (uint32_t)lane < p.B ? tiles : 0;
+    // A head's B blocks splits workgroups are dealt out by what its sequences have to do: one to each block that
+    // has tokens, the others in proportion to the block's tiles.  Lane i: sequence i.
+    it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
+    if (it >= p.items) return;
+    const uint32_t all = p.B * p.blocks * p.splits;
+    h = scalar(it / all);
+    const uint32_t j = it - h * all, seq = min((uint32_t)lane, p.B - 1);
+    const int len = p.length[seq];
+    const uint32_t tok = p.lengths ? (uint32_t)max(min(p.lengths[seq], (int)p.T), 0) : p.T;
+    const uint32_t mine = (uint32_t)lane < p.B ? 1 : 0;
+    const uint32_t tiles = mine * min(((uint32_t)max(len, 1) + kS - 1) / kS, p.ring_tiles);
+    // (the first block is there also without tokens: for the rows)
+    const uint32_t with = mine * max(p.per_head ? p.G * ((tok + QB - 1) / QB) : (p.G * tok + QB - 1) / QB, 1u);
+    auto sum_upto = [&](uint32_t x) {
 #pragma unroll
       for (int s = 1; s < 64; s *= 2) {
-        const uint32_t y = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane - s), (int)upto);
-        upto += lane >= s ? y : 0;
+        const uint32_t y = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane - s), (int)x);
+        x += lane >= s ? y : 0;
       }
-      const uint32_t others = all - p.B, before = upto - ((uint32_t)lane < p.B ? tiles : 0);
-      const float each = (float)others / (float)__builtin_amdgcn_readlane((int)upto, 63);
-      const uint32_t from = lane + min((uint32_t)((float)before * each), others);
-      const uint32_t to = lane + 1 + min((uint32_t)((float)upto * each), others);
-      b = __builtin_popcountll(__ballot((uint32_t)lane < p.B && from <= j)) - 1;
-      split = j - (uint32_t)__builtin_amdgcn_readlane((int)from, (int)b);
-      splits = (uint32_t)__builtin_amdgcn_readlane((int)to, (int)b) - (j - split);
-      if (split >= splits) return;
-    } else {
-      // (sequence, head) pairs from the longest on are dealt to the XCDs there and back, and the second half of each
-      // XCD's comes in reverse, so that workgroups that share a CU make up for one another
-      const uint32_t pairs = p.B * p.Hkv, rounds = (pairs + 7) / 8;
-      const uint32_t bid = __builtin_amdgcn_workgroup_id_x(), xcd = bid & 7;
-      uint32_t i = scalar((bid >> 3) / p.blocks);
-      blk = (bid >> 3) - i * p.blocks;
-      const uint32_t half = (rounds + 1) / 2;
-      i = i < half ? i : rounds - 1 - (i - half);
-      const uint32_t pair = i * 8 + (i & 1 ? 7 - xcd : xcd);
-      if (pair >= pairs) return;
-      const uint32_t place = scalar(pair / p.Hkv);
-      h = pair - place * p.Hkv;
-      uint32_t rank = 0;  // of sequence `lane`
-      for (uint32_t x = 0; x < p.B; ++x) {
-        const uint32_t y = (uint32_t)__builtin_amdgcn_readlane((int)tiles, (int)x);
-        rank += y > tiles || (y == tiles && x < (uint32_t)lane) ? 1 : 0;
-      }
-      b = __builtin_ctzll(__ballot((uint32_t)lane < p.B && rank == place));
-      split = 0;
-      it = 0;
+      return x;
+    };
+    const uint32_t one = scalar((uint32_t)__builtin_amdgcn_readlane((int)sum_upto(with), 63));
+    const uint32_t work = scalar((uint32_t)__builtin_amdgcn_readlane((int)sum_upto(with * tiles), 63));
+    const uint32_t each = 1 + (all - one) * tiles / work;  // (below 2^11 times 2^18)
+    const uint32_t to = sum_upto(with * each), from = to - with * each;
+    b = __builtin_popcountll(__ballot(mine && from <= j)) - 1;
+    auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)b); };
+    if (j >= of(to)) return;
+    splits = of(each);
+    const uint32_t i = j - of(from);
+    blk = scalar(i / splits);
+    split = i - blk * splits;
+    const uint32_t there = of(with), per = p.per_head ? max(scalar(there / p.G), 1u) : there;
+    if (p.per_head) {  // (the blocks with tokens come first in each head)
+      const uint32_t gh = scalar(blk / per);
+      blk = gh * p.per_head + (blk - gh * per);
     }
+    if (i == 0) bare = per;
   } else {
     it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
     if (it >= p.items) return;
@@ -255,6 +247,24 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     gh = m / per;
     t = m - gh * per + (behind ? (uint32_t)n : 0u);
   };
+
+  const int64_t row0 = (int64_t)(b * p.H + h * p.G) * p.T;
+  if (bare > 0) {  // (rows that nobody else gets to)
+    const uint32_t heads = p.per_head ? p.G : 1, from = bare * QB, rows = p.per_head ? p.T : p.M;
+    for (uint32_t gh = 0; gh < heads; ++gh)
+      for (uint32_t e = tid; from < rows && e < (rows - from) * 16; e += 64 * nw) {
+        uint32_t g_, t_, m = from + (e >> 4);
+        if (p.per_head) {
+          g_ = gh;
+          t_ = m;
+        } else {
+          place(m - m0, g_, t_);
+        }
+        const int64_t r = row0 + (int64_t)g_ * p.T + t_;
+        store4(reinterpret_cast<T*>(p.out) + r * kD + 4 * (e & 15), 0.f, 0.f, 0.f, 0.f);
+        if (p.lse && (e & 15) == 0) p.lse[r] = -INFINITY;
+      }
+  }
 
   // ---- the tree: lane i holds node i's ancestors and itself as bits
   uint64_t up = 0;
@@ -346,7 +356,6 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   }
 
   // ---- the queries: lane (g, c) takes columns 16 (g + NG x) .. of row c, x < NX
-  const int64_t row0 = (int64_t)(b * p.H + h * p.G) * p.T;
   bf16x8 qf[NC][NK][QP];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -779,11 +788,24 @@ WindowAttnPlan window_attn_plan(const gca_window& w, int64_t T) {
   return a;
 }
 
+// Where every row sees its sequence's all, some sequences may have far more to do than others: their blocks get
+// more workgroups.
+namespace {
+constexpr int kBalanceWaves = 4;  // per workgroup at least: fewer, and there are several rounds of them anyway
+bool may_balance(const gca_window& w) { return w.window == 0 && w.B > 1 && w.B <= 64 && w.capacity >= 1024; }
+bool balanced(const gca_window& w, const WindowAttnPlan& a) {
+  return may_balance(w) && a.rows <= 32 && a.waves >= kBalanceWaves;
+}
+}  // namespace
+
 size_t window_workspace(const gca_window& w, int64_t T) {
   // (what any number of row blocks of this height, or of 32, asks for: it then never falls as T grows)
   const int rows = rows_of(w, T) == 16 ? 16 : 32;
-  if (tiles_seen(w, T, rows) < 4 * kMaxWaves) return 0;
-  return align256((size_t)(kWavesPerCu * device_cus() / kMaxWaves) * rows * (kD + 2) * sizeof(float));
+  const bool balance = may_balance(w);
+  if (!balance && tiles_seen(w, T, rows) < 4 * kMaxWaves) return 0;
+  // workgroups: as many waves as fill the chip, and balanced up to twice that
+  const int64_t most = balance ? 2 * kWavesPerCu * device_cus() / kBalanceWaves : kWavesPerCu * device_cus() / kMaxWaves;
+  return align256((size_t)most * rows * (kD + 2) * sizeof(float));
 }
 
 hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t* parents, const int32_t* lengths,
@@ -825,13 +847,11 @@ hipError_t launch_window_attn(const gca_window& w, const void* q, const int32_t*
   p.negate = w.attn_scale < 0.f ? (w.dtype == GCA_BF16 ? 0x80008000u : 0x80000000u) : 0u;
   p.keep = s > 0.f ? 0xffffffffu : 0u;
   p.off_by_one = w.off_by_one;
-  // Where every row sees its sequence's all, some may have far more to do.
-  p.balance = w.window == 0 && w.B > 1 && w.B <= 64 && w.capacity >= 1024 && (a.splits == 1 || p.ticket);
+  p.balance = balanced(w, a) && p.ticket;
   size_t lds = (size_t)a.waves * 192 * sizeof(float);
   const size_t parts = a.waves * a.splits > 1 ? (size_t)a.waves * a.rows * (kD + 2) * sizeof(float) : 0;
   if (parts > lds) lds = parts;
-  const int64_t pairs = (int64_t)w.B * w.Hkv;  // (balanced without splits: whole rounds of the XCDs)
-  const dim3 grid((unsigned)(p.balance && a.splits == 1 ? (pairs + 7) / 8 * 8 * a.blocks : (p.items + 7) / 8 * 8));
+  const dim3 grid((p.items + 7) / 8 * 8);
   const dim3 block(64 * a.waves);
   auto run = [&](auto tag, auto i8) {
     using T_ = decltype(tag);
