@@ -144,7 +144,7 @@ def _clean(x):
 
 
 def _whole(r):
-    return np.rint(r * FIX).astype(np.int64)
+    return np.rint(r * FIX).astype(np.uint64)
 
 
 def verify(p, tokens, u, q=None, parents=None, lengths=None):
@@ -186,6 +186,6 @@ def verify(p, tokens, u, q=None, parents=None, lengths=None):
             w = _whole(_clean(p[b, a]))
         total = int(w.sum())
         if total:
-            at = int(np.floor(uu[b, 0] * float(total)))
-            nxt[b] = int(np.searchsorted(np.cumsum(w), at, side="right"))
+            at = np.uint64(np.floor(uu[b, 0] * float(total)))
+            nxt[b] = int(np.searchsorted(np.cumsum(w, dtype=np.uint64), at, side="right"))
     return path, count, nxt

@@ -5,8 +5,8 @@
 // min(1, r[x] / (z q[x])); a rejection leaves r <- max(r - z q, 0), z <- sum r.  (r / z is then the
 // distribution that the next child, drawn from q too, has to make up for; with the draw from r at
 // the end each token comes out with probability p[a].)  Children that were chosen rather than drawn are q = 1
-// at x.  Everything is fp64 without contraction, and sums are of whole multiples of 2^-44 in 64-bit integers
-// (2^19 entries of at most 1 stay below 2^63), so that results do not depend on how the work is cut.
+// at x.  Everything is fp64 without contraction, and sums are of whole multiples of 2^-44 in 64-bit unsigned
+// integers (2^19 entries of at most 1 are at most 2^63), so that results do not depend on how the work is cut.
 //
 // Work.  One lane per node holds the node's token and its entries of p and q, so that the walk is
 // comparisons and ballots after two dependent loads.  The vocabulary is cut into slices, one
@@ -48,7 +48,7 @@ struct VerifyParams {
   int32_t* count;
   int32_t* next;
   Walk* walk;      // [B]
-  int64_t* sums;   // [B][slices][waves]
+  uint64_t* sums;   // [B][slices][waves]
   uint32_t B, T, slices;
   uint32_t V, per;  // entries in all, and per wave of a slice (a multiple of 4)
 };
@@ -73,9 +73,9 @@ __device__ __forceinline__ bool test(double u, double z, double q, double r) {
 }
 // r in whole multiples of 2^-44, to the nearest (ties to even): 0 .. 2^44, so the sum with 2^52 holds it
 // in its mantissa.
-__device__ __forceinline__ int64_t whole(double r) {
+__device__ __forceinline__ uint64_t whole(double r) {
   const double x = r * kFix + 4503599627370496.0;
-  return __double_as_longlong(x) & 0xfffffffffffffll;
+  return (uint64_t)__double_as_longlong(x) & 0xfffffffffffffull;
 }
 
 // Lane c's value, c the same in every lane.
@@ -87,7 +87,7 @@ __device__ __forceinline__ double lane_of(double x, int c) {
   return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+__device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) x += __shfl_xor(x, s);
   return x;
@@ -99,7 +99,7 @@ typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4u;
 // `chosen`: of the rejected tokens too.
 template <int N>
 __device__ __forceinline__ void left(const Walk& w, bool drawn, bool chosen, const float* p, const float* q, uint32_t x,
-                                     int64_t* out) {
+                                     uint64_t* out) {
   double r[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) r[e] = prob(p[e]);
@@ -122,12 +122,12 @@ __device__ __forceinline__ void left(const Walk& w, bool drawn, bool chosen, con
 
 // Part `part` of `parts` (lanes or threads) of the sum of r over entries [lo, hi) of the last node's row, four
 // consecutive entries at a time; `plain`: of p[a] itself.
-__device__ __forceinline__ int64_t part_sum(const VerifyParams& p, const Walk& w, uint32_t b, uint32_t lo, uint32_t hi,
+__device__ __forceinline__ uint64_t part_sum(const VerifyParams& p, const Walk& w, uint32_t b, uint32_t lo, uint32_t hi,
                                             bool plain, uint32_t part, uint32_t parts) {
   const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
   const float* pr = p.p + row;
   const bool drawn = p.q != nullptr && w.rejected > 0 && !plain;
-  int64_t sum = 0;
+  uint64_t sum = 0;
   uint32_t x = lo + 4 * part;
   if (drawn) {
     const float* qr = p.q + row;
@@ -135,12 +135,12 @@ __device__ __forceinline__ int64_t part_sum(const VerifyParams& p, const Walk& w
     for (; x + 4 <= hi; x += 4 * parts) {
       const f32x4u a = *reinterpret_cast<const f32x4u*>(pr + x), c = *reinterpret_cast<const f32x4u*>(qr + x);
       const float pe[4] = {a[0], a[1], a[2], a[3]}, qe[4] = {c[0], c[1], c[2], c[3]};
-      int64_t r[4];
+      uint64_t r[4];
       left<4>(w, true, false, pe, qe, x, r);
       sum += r[0] + r[1] + r[2] + r[3];
     }
     for (; x < hi; ++x) {
-      int64_t r;
+      uint64_t r;
       left<1>(w, true, false, pr + x, qr + x, x, &r);
       sum += r;
     }
@@ -163,22 +163,22 @@ __device__ __forceinline__ int64_t part_sum(const VerifyParams& p, const Walk& w
 }
 
 // Sum over the workgroup, to every thread.
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* lds) {
+__device__ __forceinline__ uint64_t block_sum(uint64_t x, uint64_t* lds) {
   x = wave_sum(x);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
   __syncthreads();
-  int64_t s = 0;
+  uint64_t s = 0;
 #pragma unroll
   for (int w = 0; w < kVerifyWaves; ++w) s += lds[w];
   return s;
 }
 // Sum of the threads up to this one, and of all.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* lds, int64_t& all) {
+__device__ __forceinline__ uint64_t block_scan(uint64_t x, uint64_t* lds, uint64_t& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
-    const int64_t y = __shfl_up(x, s);
+    const uint64_t y = __shfl_up(x, s);
     if (lane >= s) x += y;
   }
   __syncthreads();
@@ -194,7 +194,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* lds, int64_t& 
 }
 
 // The walk of sequence b into w, by the whole workgroup.
-__device__ __forceinline__ void walk_tree(const VerifyParams& p, uint32_t b, Walk& w, int& again, int64_t* lds) {
+__device__ __forceinline__ void walk_tree(const VerifyParams& p, uint32_t b, Walk& w, int& again, uint64_t* lds) {
   const int lane = threadIdx.x & 63;
   const bool first_wave = threadIdx.x < 64, drawn = p.q != nullptr;
 
@@ -286,7 +286,7 @@ __device__ __forceinline__ void walk_tree(const VerifyParams& p, uint32_t b, Wal
     }
     __syncthreads();
     if (!again) break;
-    const int64_t s = block_sum(part_sum(p, w, b, 0, p.V, false, threadIdx.x, kVerifyThreads), lds);
+    const uint64_t s = block_sum(part_sum(p, w, b, 0, p.V, false, threadIdx.x, kVerifyThreads), lds);
     z = (double)s * kUnfix;
     __syncthreads();  // (`again` and the walk are read before they are written again)
   }
@@ -305,7 +305,7 @@ __device__ __forceinline__ void write_path(const VerifyParams& p, uint32_t b, co
 
 __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParams p) {
   __shared__ Walk w;
-  __shared__ int64_t lds[kVerifyWaves];
+  __shared__ uint64_t lds[kVerifyWaves];
   __shared__ int again;
   const uint32_t b = blockIdx.x / p.slices, slice = blockIdx.x - b * p.slices;
   const int lane = threadIdx.x & 63;
@@ -320,19 +320,19 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_walk_kernel(VerifyParam
   // one sum per wave, each of a quarter of the slice
   const uint32_t quarter = slice * kVerifyWaves + (threadIdx.x >> 6);
   const uint32_t lo = min(quarter * p.per, p.V), hi = min(lo + p.per, p.V);
-  const int64_t s = wave_sum(part_sum(p, w, b, lo, hi, false, lane, 64));
+  const uint64_t s = wave_sum(part_sum(p, w, b, lo, hi, false, lane, 64));
   if (lane == 0) p.sums[(int64_t)b * p.slices * kVerifyWaves + quarter] = s;
 }
 
 // The first entry of [lo, hi) of the last node's row whose partial sum from lo on exceeds `place`; `plain`: of
 // p[a] itself.  kPerThread consecutive entries per thread.
 __device__ __forceinline__ void draw(const VerifyParams& p, const Walk& w, uint32_t b, uint32_t lo, uint32_t hi,
-                                     int64_t place, bool plain, int64_t* lds) {
+                                     uint64_t place, bool plain, uint64_t* lds) {
   const int64_t row = ((int64_t)b * p.T + w.node) * p.V;
   const bool drawn = p.q != nullptr && w.rejected > 0;
   const float* pr = p.p + row;
   const float* qr = drawn ? p.q + row : pr;
-  int64_t before = 0;
+  uint64_t before = 0;
   for (uint32_t x0 = lo; x0 < hi; x0 += kVerifyThreads * kPerThread) {
     const uint32_t x = x0 + threadIdx.x * kPerThread;
     float pe[kPerThread], qe[kPerThread];
@@ -353,17 +353,17 @@ __device__ __forceinline__ void draw(const VerifyParams& p, const Walk& w, uint3
         qe[e] = x + e < p.V ? qr[x + e] : 0.f;
       }
     }
-    int64_t r[kPerThread], mine = 0;
+    uint64_t r[kPerThread], mine = 0;
     left<kPerThread>(w, drawn && !plain, p.q == nullptr && !plain, pe, qe, x, r);
 #pragma unroll
     for (int e = 0; e < kPerThread; ++e) {
       r[e] = x + e < hi ? r[e] : 0;
       mine += r[e];
     }
-    int64_t step;
-    const int64_t upto = before + block_scan(mine, lds, step);
+    uint64_t step;
+    const uint64_t upto = before + block_scan(mine, lds, step);
     if (upto > place && upto - mine <= place) {  // one thread
-      int64_t at = upto - mine;
+      uint64_t at = upto - mine;
       uint32_t found = x;
 #pragma unroll
       for (int e = 0; e < kPerThread; ++e) {
@@ -381,13 +381,13 @@ __device__ __forceinline__ void draw(const VerifyParams& p, const Walk& w, uint3
 // per thread, and the token in it.
 __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParams p) {
   __shared__ Walk w;
-  __shared__ int64_t lds[kVerifyWaves];
-  __shared__ int64_t place;
+  __shared__ uint64_t lds[kVerifyWaves];
+  __shared__ uint64_t place;
   __shared__ uint32_t chosen;
   const uint32_t b = blockIdx.x, tid = threadIdx.x;
   float u = p.u[(int64_t)b * p.T];
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-  int64_t part[kVerifyWaves];
+  uint64_t part[kVerifyWaves];
 #pragma unroll
   for (int e = 0; e < kVerifyWaves; ++e)
     part[e] = tid < p.slices ? p.sums[((int64_t)b * p.slices + tid) * kVerifyWaves + e] : 0;
@@ -398,13 +398,13 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParam
     if (tid == 0) p.next[b] = -1;
     return;
   }
-  int64_t mine = 0, total;
+  uint64_t mine = 0, total;
 #pragma unroll
   for (int e = 0; e < kVerifyWaves; ++e) mine += part[e];
-  const int64_t upto = block_scan(mine, lds, total);
+  const uint64_t upto = block_scan(mine, lds, total);
   uint32_t lo = 0, hi = p.V;
   bool plain = false;
-  int64_t at;
+  uint64_t at;
   if (total == 0) {  // nothing is left: of p itself, the whole vocabulary as one part
     plain = true;
     total = block_sum(part_sum(p, w, b, 0, p.V, true, tid, kVerifyThreads), lds);
@@ -412,9 +412,9 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyParam
       if (tid == 0) p.next[b] = -1;
       return;
     }
-    at = (int64_t)((double)u * (double)total);
+    at = (uint64_t)((double)u * (double)total);
   } else {
-    at = (int64_t)((double)u * (double)total);
+    at = (uint64_t)((double)u * (double)total);
     if (upto > at && upto - mine <= at) {  // one thread
       at -= upto - mine;
       uint32_t e = 0;
@@ -453,7 +453,7 @@ VerifyPlan verify_plan(int64_t B, int64_t V) {
 size_t verify_workspace(int64_t B, int64_t T, int64_t V) {
   (void)T;
   const VerifyPlan a = verify_plan(B, V);
-  return align256((size_t)B * sizeof(Walk)) + align256((size_t)B * a.slices * kVerifyWaves * sizeof(int64_t));
+  return align256((size_t)B * sizeof(Walk)) + align256((size_t)B * a.slices * kVerifyWaves * sizeof(uint64_t));
 }
 
 hipError_t launch_verify(int64_t B, int64_t T, int64_t V, const float* p, const float* q, const int32_t* tokens,
@@ -471,7 +471,7 @@ hipError_t launch_verify(int64_t B, int64_t T, int64_t V, const float* p, const 
   k.count = count;
   k.next = next;
   k.walk = static_cast<Walk*>(ws);
-  k.sums = reinterpret_cast<int64_t*>(static_cast<char*>(ws) + align256((size_t)B * sizeof(Walk)));
+  k.sums = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + align256((size_t)B * sizeof(Walk)));
   k.B = (uint32_t)B;
   k.T = (uint32_t)T;
   k.slices = (uint32_t)a.slices;

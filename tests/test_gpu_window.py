@@ -348,3 +348,22 @@ def test_verify_odd_probabilities(dev, gca):
         for x, y, name in zip(got, want, ("path", "count", "next")):
             assert np.array_equal(x.cpu().numpy(), y), name
         assert (got[2][3] == -1).item() and (got[2][4] == -1).item()
+
+
+@pytest.mark.parametrize("with_q", [False, True])
+def test_verify_of_the_largest_sum(dev, gca, with_q):
+    """2^19 probabilities of 1 are 2^63 in whole multiples of 2^-44.  (With a first draft that q does not have, and so
+    is accepted, or with drafts that leave p as it is: their tokens are no tokens.)"""
+    import torch
+    B, T, V = 3, 3, 1 << 19
+    p = np.ones((B, T, V), np.float32)
+    q = np.zeros((B, T, V), np.float32) if with_q else None
+    tok = np.array([[0, -1, V], [0, 5, -1], [0, V - 1, 7]], np.int32)
+    par = np.array([[-1, 0, 0]] * B, np.int32)
+    u = np.array([[0.75, 0.5, 0.5], [0.0, 0.25, 0.5], [1 - 2.0**-24, 0.9, 0.9]], np.float32)
+    up = lambda x: None if x is None else torch.from_numpy(x).to(dev)  # noqa: E731
+    got = gca.verify(up(p), up(tok), up(u), q=up(q), parents=up(par))
+    want = ow.verify(p, tok, u, q, par)
+    assert want[2][0] == 3 << 17
+    for x, y, name in zip(got, want, ("path", "count", "next")):
+        assert np.array_equal(x.cpu().numpy(), y), name

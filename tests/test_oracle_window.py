@@ -109,3 +109,6 @@ def test_verify_closed_forms():
     assert [draw(x, 3, q) for x in (0.49, 0.51)] == [0, 2]
     # nothing left: of p itself
     assert draw(0.9, 3, half * 0 + 1.0) == 3
+    # the largest sum, 2^19 ones in whole multiples of 2^-44: 2^63
+    ones = np.ones((1, 1, 1 << 19), np.float32)
+    assert ow.verify(ones, np.array([[0]]), np.array([[0.75]], np.float32))[2].tolist() == [3 << 17]
