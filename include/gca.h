@@ -439,11 +439,13 @@ gca_status gca_window_attn(const gca_window* w, const void* q, const int32_t* pa
 
 /* Of the newest n_b = lengths[b] (NULL: T) tokens keep those that path names, in its order, and drop the
  * others: token path[b, i] moves to position base + i, base = length[b] - n_b, and length[b] becomes
- * base + m.  The path's m entries end at the first that is not larger than the one before, or is
- * outside 0 .. n_b - 1 (-1 padding).
+ * base + m.  The path's m entries end at the first that is not larger than the one before, is
+ * outside 0 .. n_b - 1 (-1 padding), or (window = 0) would bring a token from past the capacity, which was
+ * not kept, below it.
  *   path    [B, n] int32, 0 <= n <= 64 (e.g. from gca_verify)
  *   lengths [B]    int32, as for the append; may be NULL
- * Requires w->k, v, k_scale, v_scale, length, ticket.  T >= 1; in a ring T <= capacity. */
+ * Requires w->k, v, k_scale, v_scale, length, ticket.  T >= 1; in a ring window + T - 1 <= capacity, as for the
+ * attention: the rows of dropped tokens then held none that the next ones see. */
 gca_status gca_window_keep(const gca_window* w, const int32_t* path, int64_t n, const int32_t* lengths, int64_t T,
                            hipStream_t stream);
 

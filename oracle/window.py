@@ -56,7 +56,7 @@ def keep(w, path, lengths, T, window):
     for b in range(B):
         base, last, m = max(0, int(w["length"][b] - n[b])), -1, 0
         for x in path[b]:
-            if x <= last or x >= n[b]:
+            if x <= last or x >= n[b] or (not window and base + x >= C and base + m < C):
                 break
             last, m = x, m + 1
         for i in range(m):

@@ -128,7 +128,9 @@ gca_status gca_window_keep(const gca_window* w, const int32_t* path, int64_t n, 
   GCA_TRY(check_tokens(w, T));
   if (n < 0) return fail(GCA_ERR_INVALID, "n must be >= 0");
   if (n > gca::kTreeNodes) return fail(GCA_ERR_UNSUPPORTED, "a path has at most 64 entries");
-  if (w->window > 0 && T > w->capacity) return fail(GCA_ERR_INVALID, "T must be <= capacity");
+  // (a dropped token's row was another's, which a row behind what is kept may see)
+  if (w->window > 0 && w->window + T - 1 > w->capacity)
+    return fail(GCA_ERR_INVALID, "window + T - 1 must be <= capacity");
   GCA_TRY(check_rows(w));
   GCA_TRY(check_ptr(path, "path", n > 0, 4));
   GCA_TRY(check_ptr(lengths, "lengths", false, 4));

@@ -277,9 +277,11 @@ __global__ __launch_bounds__(kKeepWaves * 64) void window_keep_kernel(KeepParams
   // lane i: entry i, in the path if every entry up to it is larger than the one before
   const int mine = lane < (int)p.n ? p.path[(int64_t)b * p.n + lane] : -1;
   const int left = __shfl_up(mine, 1);  // (by every lane: one that is not active has nothing to give)
-  const uint64_t good = __ballot(mine > (lane ? left : -1) && mine < n);
-  const int m = good == ~0ull ? 64 : __builtin_ctzll(~good);
   const int64_t base = length > n ? length - n : 0;
+  // (no token past the capacity comes below it: it has no numbers)
+  const bool lost = !p.ring && base + mine >= p.C && base + lane < p.C;
+  const uint64_t good = __ballot(mine > (lane ? left : -1) && mine < n && !lost);
+  const int m = good == ~0ull ? 64 : __builtin_ctzll(~good);
   const uint32_t h = part * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // entries that name their own place lead the path and stay
   const uint64_t moved = __ballot(lane < m && mine != lane);

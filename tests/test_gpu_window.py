@@ -278,6 +278,19 @@ def test_keep(dev, gca, window, C, fmt):
         _same(w, ref, "e4m3")
 
 
+def test_keep_ends_where_a_token_was_not_kept(dev, gca):
+    """As the oracle's: in a window of 64 rows, tokens from position 64 on have none."""
+    import torch
+    for path in ([0, 2, 3, 5], [0, 1, 2, 3, 5], [4], [0, 1, 2, 3, 4, 5], [5]):
+        w = gca.window(3, 2, 64, device=dev)
+        _fill(w, 9, [66, 60, 70])
+        ref = _state(w)
+        p = np.array([path] * 3, np.int32)
+        gca.window_keep(w, 6, torch.from_numpy(p).to(dev))
+        ow.keep(ref, p, None, 6, 0)
+        _same(w, ref, "e4m3")
+
+
 def _drafts(rng, B, T, V, kind, with_q):
     p = rng.standard_normal((B, T, V)) * 2
     q = p + rng.standard_normal((B, T, V)) * (0.5 if kind != "far" else 4.0)

@@ -73,6 +73,18 @@ def test_append_wraps_and_keeps_the_last():
         assert (w["v"][0, 0, 0, :, p % 64] == w["k"][0, 0, p % 64]).all()
 
 
+def test_keep_ends_where_a_token_was_not_kept():
+    """C = 64 and 60 tokens before: tokens 4 and on of the new ones have no rows."""
+    for path, m in (([0, 2, 3, 5], 3), ([0, 1, 2, 3, 5], 5), ([4], 0), ([0, 1, 2, 3, 4, 5], 6)):
+        w = _window(np.random.default_rng(1), 1, 1, 64)
+        w["length"][:] = 66
+        old = w["k"].copy()
+        ow.keep(w, np.array([path]), None, 6, 0)
+        assert w["length"][0] == 60 + m
+        for i in range(min(m, 4)):
+            assert (w["k"][0, 0, 60 + i] == old[0, 0, 60 + path[i]]).all()
+
+
 @pytest.mark.parametrize("children,drawn", [(1, True), (2, True), (3, True), (1, False), (2, False)])
 def test_verified_tokens_follow_the_target(children, drawn):
     """The token behind the root, accepted or drawn, has probability p[0] whatever the draft's q: in n

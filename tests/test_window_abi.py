@@ -122,6 +122,7 @@ def test_counts_are_refused(gca):
     # a ring's window has to outlast the new tokens
     assert _attn(gca, w, T=514) == gca.GCA_ERR_INVALID and "capacity" in _msg(gca)
     assert _keep(gca, w, T=1025) == gca.GCA_ERR_INVALID
+    assert _keep(gca, w, T=514) == gca.GCA_ERR_INVALID and "capacity" in _msg(gca)
     assert _attn(gca, w, T=65, parents=FAKE) == gca.GCA_ERR_UNSUPPORTED
     assert _keep(gca, w, n=65) == gca.GCA_ERR_UNSUPPORTED
     assert _keep(gca, w, n=-1) == gca.GCA_ERR_INVALID
