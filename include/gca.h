@@ -382,7 +382,8 @@ size_t gca_cache_workspace_size(const gca_cache* c, int op, int64_t n);
  * (values) has the scale NaN for its keys (values).
  *
  * B sequences; H query heads share Hkv cached heads, as in gca_cache.  Supported: d == 64, H a
- * multiple of Hkv, capacity a multiple of 64 up to 2^24, window 0 .. capacity. */
+ * multiple of Hkv, B H < 2^19, capacity a multiple of 64 up to 2^24, window 0 .. capacity, and
+ * calls of T tokens with B H T up to 2^26. */
 typedef struct {
   int32_t B, H, Hkv;
   int32_t d;
@@ -429,8 +430,10 @@ gca_status gca_window_append(const gca_window* w, const void* k, const void* v, 
  * In a ring, a row's window has to outlast the new tokens: window + T - 1 <= capacity (a
  * longer prompt comes in pieces; GCA_ERR_INVALID).  Products of q with the kept numbers are exact and summed
  * in fp32.  Probabilities relative to the row's largest so far, with their value scale in them, are rounded to
- * fp16 (fp32 tensors: to two fp16 terms), but not finer than to a 2^-40th of the largest
- * value scale that the row's block of rows has met.
+ * fp16 (fp32 tensors: to two fp16 terms): by 2^-11 (2^-22) of themselves, or, where they are so small, by up to a
+ * 2^-39th of the largest value scale that the row's block of rows has met.  (Blocks of 64 rows, for
+ * GCA_E4M3 and bf16 where there are enough to fill the chip, round the probabilities alone, by 2^-11 or 2^-40, and
+ * hold values in fp16, exactly, or, where they are so small, to a 2^-30th of that scale.)
  * Requires w->k, v, k_scale, v_scale, length, ticket.  Workspace: gca_window_workspace_size(w, T)
  * bytes, 256-byte aligned. */
 gca_status gca_window_attn(const gca_window* w, const void* q, const int32_t* parents, const int32_t* lengths,

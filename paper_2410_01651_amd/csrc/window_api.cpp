@@ -36,7 +36,7 @@ gca_status check_window(const gca_window* w) {
   if (w->off_by_one != 0 && w->off_by_one != 1) return fail(GCA_ERR_INVALID, "off_by_one must be 0 or 1");
   if (w->flags != 0) return fail(GCA_ERR_INVALID, "unknown flag bits");
   if (!std::isfinite(w->attn_scale)) return fail(GCA_ERR_INVALID, "scales must be finite");
-  if ((int64_t)w->B * w->H > kMaxItems / 256) return fail(GCA_ERR_UNSUPPORTED, "window too large for one launch");
+  if ((int64_t)w->B * w->H > kMaxItems / 16) return fail(GCA_ERR_UNSUPPORTED, "window too large for one launch");
   return GCA_OK;
 }
 
@@ -49,7 +49,7 @@ gca_status check_rows(const gca_window* w) {
   return check_ptr(w->ticket, "window ticket", true, 4);
 }
 
-// T new tokens of every sequence (bounds before products: B * H is at most 2^15).
+// T new tokens of every sequence (bounds before products: B * H is below 2^19).
 gca_status check_tokens(const gca_window* w, int64_t T) {
   if (T < 1) return fail(GCA_ERR_INVALID, "T must be >= 1");
   if (T > 0x40000000 || T > kMaxItems / ((int64_t)w->B * w->H) * 16)

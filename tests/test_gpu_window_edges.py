@@ -137,6 +137,28 @@ def test_scores_and_scales_at_the_ends_of_their_range(dev, gca):
                                None, None, sl)
 
 
+@pytest.mark.parametrize("T,G,tree", [(1, 33, False), (40, 1, True), (64, 1, False)])
+def test_scales_far_apart_in_blocks_of_64_rows(dev, gca, T, G, tree):
+    """So many sequences that blocks have 64 rows, and value scales from 2^-20 to 2^20, the largest ones among the
+    oldest tokens or the newest; three of the sequences are compared."""
+    import torch
+    from types import SimpleNamespace
+    B, Hkv, C = 256, 8, 128
+    w = gca.window(B, Hkv * G, C, Hkv=Hkv, device=dev)
+    g = tw._fill(w, 21, [C] * B)
+    q = torch.randn(B, Hkv * G, T, 64, generator=g, device=dev).to(torch.bfloat16)
+    par = torch.from_numpy(tw._tree(np.random.default_rng(2), B, T, "random")).to(dev) if tree else None
+    sl = torch.full((Hkv * G,), 0.5, device=dev)
+    for turned in (False, True):
+        e = torch.linspace(20, -20, C, device=dev).round()
+        w.v_scale.copy_(torch.exp2(e.flip(0) if turned else e))
+        out, lse = gca.window_attn(w, q, parents=par, slopes=sl)
+        for b in (0, 100, B - 1):
+            one = SimpleNamespace(struct=w.struct, **{n: getattr(w, n)[b:b + 1] for n in w.NAMES})
+            tw._check_attn(one, q[b:b + 1], (out[b:b + 1], lse[b:b + 1]), None if par is None else par[b:b + 1], None, sl,
+                           held=2.0**20)
+
+
 def _step(gca, w, k, v, q, par, p, qd, tok, u, ws):
     """A step of a serving loop: the drafts join the window, attend, are verified, and the accepted path stays."""
     gca.window_append(w, k, v)
