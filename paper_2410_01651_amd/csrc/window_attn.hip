@@ -18,7 +18,16 @@
 // handed round through 512 bytes of LDS per wave.
 //
 // Work.  One item per (sequence, cached head, block of rows); its waves, of one or more workgroups, take the
-// tiles in turn and leave (m, l, out) to be joined.
+// tiles in turn and leave (m, l, out) to be joined, by the workgroup through LDS, and for several workgroups by
+// the last of them through memory.  No wave waits for another's tile: there is no barrier before the join.
+//
+// Bound.  Few rows per cached head (single tokens, small trees): HBM, 136 bytes per token and cached head.  One
+// token of 64 sequences, 16 heads, a window of 512: 15 us (71.6 MB, 4.8 TB/s); of four sequences of up to 120,000
+// tokens, 8 cached heads for 32: 76 us (411 MB, 5.4 TB/s).  Many rows (prompts): instruction issue, of which the
+// softmax has most: a tile of 64 x 64 takes 610 vector instructions beside its 32 MFMA.  8,192 tokens of 4
+// sequences, 16 heads, a window of 512: 125 us, vector pipes busy 68 %, MFMA 24 %.  A tree of 25 nodes over 8 cached heads for 32 heads, 16
+// sequences of up to 7,777 tokens: 40 us; four blocks of 32 rows unpack each tile, and vector pipes are busy 33 %.
+// One sequence's token of 8 heads over 512: 6 us, the trips to memory (length, tile, parts) one after the other.
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
 #include "numbers8.hpp"
@@ -79,7 +88,11 @@ __device__ __forceinline__ Joined finish(float m, float l, int off_by_one) {
 }
 
 // Parts of a split row block go through memory that every XCD sees: two floats written and read past the
-// caches that each XCD has for itself.
+// caches that each XCD has for itself (agent scope), so that nothing else in those caches is written back or
+// dropped: the ticket is drawn once every store of the workgroup has been acknowledged (a wait of each thread,
+// then the barrier), and read back after it, by loads that go where the stores went.  With fences of agent
+// scope around the ticket instead, four sequences of up to 120,000 tokens take 120 us for 77, 16 sequences' trees of
+// 25 nodes 59 for 40.
 __device__ __forceinline__ void put2(float* at, float x, float y) {
   const uint64_t u = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
   __hip_atomic_store(reinterpret_cast<uint64_t*>(at), u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -161,7 +174,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
   // item = ((b Hkv + h) blocks + block) splits + split, unless the sequences' lengths have a say
   uint32_t b, h, blk, split, splits = p.splits, it;
-  uint32_t bare = 0;  // blocks from here on (of each head, cut head by head) that have no tokens, 0: none to be written here
+  uint32_t bare = 0;  // blocks from here on (of each head, cut head by head) have no tokens; 0: not this one's to write
   if (p.balance) {
     // A head's B blocks splits workgroups are dealt out by what its sequences have to do: one to each block that
     // has tokens, the others in proportion to the block's tiles.  Lane i: sequence i.
@@ -725,7 +738,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   __syncthreads();
   if (*drawn != splits - 1) return;
   if (tid == 0) __hip_atomic_store(p.ticket + bb, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw) 
+  for (uint32_t e = tid; e < nrows * 16; e += 64 * nw)
     join_rows<T, QB>(p, it - split, splits, e >> 4, e & 15, row0 + row_of(e >> 4));
 }
 
@@ -753,9 +766,14 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
 }  // namespace
 
 namespace {
+// Waves that a launch is cut into where its row blocks are fewer.  8 / 16 / 32 per CU: 64 sequences' single tokens
+// 15.1 / 16.0 / 18.2 us, four long sequences' 79 / 82 / 85, trees of 25 nodes 54 / 67 / 82: each wave has two
+// tiles on their way, and more waves are more parts to join.
 constexpr int kWavesPerCu = 8;
 // 64 rows unpack a tile for twice the rows, but leave two waves per SIMD: where such blocks, a wave each, fill
-// the chip.
+// the chip.  64 / 32 rows there: a prompt of 8,192 tokens 126 / 141 us.  Short of that: the tree of 25 nodes
+// 55 / 52, one of 10 nodes 37 / 32, 64 tokens of two sequences 13.8 / 8.1.  int8, whose numbers have no scaled
+// conversion, would spill: prompt 315 / 175, tree 95 / 66.
 int rows_of(const gca_window& w, int64_t T) {
   const int64_t G = w.H / w.Hkv, M = G * T, blocks = T >= 64 ? G * ((T + 63) / 64) : (M + 63) / 64;
   if (M <= 16) return 16;
@@ -790,7 +808,8 @@ WindowAttnPlan window_attn_plan(const gca_window& w, int64_t T) {
 }
 
 // Where every row sees its sequence's all, some sequences may have far more to do than others: their blocks get
-// more workgroups.
+// more workgroups.  The tree of 25 nodes over 16 sequences of 1 to 7,777 tokens: 54 us with as many for each,
+// 40 so; of equal lengths 33 either way.  (In workgroups of two waves 38, but of equal lengths 38.)
 namespace {
 constexpr int kBalanceWaves = 4;  // per workgroup at least: fewer, and there are several rounds of them anyway
 bool may_balance(const gca_window& w) { return w.window == 0 && w.B > 1 && w.B <= 64 && w.capacity >= 1024; }
