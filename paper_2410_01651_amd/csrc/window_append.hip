@@ -9,7 +9,9 @@
 // writes its own rows and no others.  Few tokens are taken eight to a wave instead, a row for eight lanes, and are
 // read before the length that says where they go is there: 64 sequences' single tokens of 16 heads 5.0 us for 6.0.
 // Bound: few tokens by the trips to memory; many by HBM, at 2 B Hkv T (64 (e + 1) + 4) bytes: four prompts of
-// up to 8,192 tokens, 16 heads, 103 MB in 24 us, 4.3 TB/s.
+// up to 8,192 tokens, 16 heads, 113 MB in 22.7 us, 5.0 TB/s, as a large copy, where the last cache still has
+// what was just computed, and 121 MB in 30.6 us, 3.9 TB/s, where it has not.  (Loads that leave that cache alone:
+// 27.0 us there, but 25.6 for the 22.7.)
 //
 // Keep.  One wave per (sequence, cached head), eight tokens at a time (64 sequences' paths, 16 heads, 6.9 us for
 // 15.3 one by one); lane d moves key d and value d of each token.  As a path ascends, token i comes from a place at
@@ -37,7 +39,7 @@ struct AppendParams {
   int64_t T, C;
   uint32_t seqs, per;    // sequences; workgroups of each
   uint32_t items;        // waves' items of a sequence: Hkv tiles 2
-  uint32_t tiles, Hkv, stride;  // stride: tickets of a sequence
+  uint32_t tiles, Hkv, stride;  // tiles of 64 (8) tokens of a sequence and head; tickets of a sequence
   int ring;
 };
 
@@ -137,13 +139,13 @@ __device__ __forceinline__ int64_t last_kept(const AppendParams& p, int64_t leng
   return p.ring || length + n <= p.C ? n : p.C - length;
 }
 
-// Many tokens: one tile of rows.
+// Many tokens: one tile of rows, of `tiles` of the sequence and head.
 template <typename T, bool I8>
-__device__ __forceinline__ void append_tile(const AppendParams& p, uint32_t b, uint32_t item, int64_t length,
-                                            int64_t n, int lane) {
+__device__ __forceinline__ void append_tile(const AppendParams& p, uint32_t b, uint32_t item, uint32_t tiles,
+                                            int64_t length, int64_t n, int lane) {
   // item = (h tiles + t) 2 + which
   const uint32_t which = item & 1;
-  const uint32_t h = __builtin_amdgcn_readfirstlane((item >> 1) / p.tiles), t = (item >> 1) - h * p.tiles;
+  const uint32_t h = __builtin_amdgcn_readfirstlane((item >> 1) / tiles), t = (item >> 1) - h * tiles;
   const int64_t i0 = first_kept(p, n), i1 = last_kept(p, length, n);
   const int64_t first = ((length + i0) / kS + t) * kS;  // the tile's first position
   int64_t lo = length + i0 - first, hi = length + i1 - first;  // its rows [lo, hi)
@@ -186,10 +188,11 @@ __device__ __forceinline__ void append_tile(const AppendParams& p, uint32_t b, u
   uint8_t* dst = p.dst[which] + row0 * kD + (which ? cg * 8 * kS + rg * 8 : rg * 8 * kD + cg * 8);
   const int from = max((int)lo - 8 * rg, 0), to = min((int)hi - 8 * rg, 8);  // this lane's rows
   if (which && (from > 0 || to < 8)) {
-    for (int r = from; r < to; ++r)
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        dst[c * kS + r] = (uint8_t)((r < 4 ? w[2 * c] : w[2 * c + 1]) >> (8 * (r & 3)));
+    for (int r = 0; r < 8; ++r)
+      if (r >= from && r < to)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) dst[c * kS + r] = (uint8_t)(w[2 * c + (r >> 2)] >> (8 * (r & 3)));
   } else {
 #pragma unroll
     for (int r = 0; r < 8; ++r)
@@ -241,19 +244,59 @@ __device__ __forceinline__ void update_length(int32_t* length, int32_t* ticket, 
   if (last) *length = (int32_t)(now < 0x7fffffff ? now : 0x7fffffff);
 }
 
-template <typename T, bool I8, bool FEW>
-__global__ __launch_bounds__(FEW ? 1024 : kAppendWaves * 64) void window_append_kernel(AppendParams p) {
-  const uint32_t b = blockIdx.x / p.per, part = blockIdx.x - b * p.per;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t waves = blockDim.x >> 6;
-  const int64_t length = max((int)__builtin_amdgcn_readfirstlane(p.length[b]), 0);
-  const int64_t n = new_tokens(p.lengths, b, p.T);
-  for (uint32_t item = part * waves + wave; item < p.items; item += p.per * waves) {
-    if constexpr (FEW) append_few<T, I8>(p, b, item, threadIdx.x & 63);
-    else append_tile<T, I8>(p, b, item, length, n, threadIdx.x & 63);
+// Many tokens of at most 64 sequences: every workgroup goes over the tiles of all of them; lane i holds sequence i's.
+template <typename T, bool I8>
+__device__ __forceinline__ void append_all(const AppendParams& p) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const uint32_t seq = min((uint32_t)lane, p.seqs - 1);
+  const int length = max(p.length[seq], 0), n = (int)new_tokens(p.lengths, seq, p.T);
+  const int64_t i0 = first_kept(p, n), i1 = last_kept(p, length, n);
+  const bool any = (uint32_t)lane < p.seqs && i1 > i0;
+  const uint32_t tiles = any ? (uint32_t)((length + i1 - 1) / kS - (length + i0) / kS + 1) : 0;
+  const uint32_t mine = tiles * p.Hkv * 2;
+  uint32_t to = mine;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const uint32_t y = (uint32_t)__shfl_up((int)to, s);
+    to += lane >= s ? y : 0;
   }
-  __syncthreads();  // (the workgroup's waves have read the length)
-  if (threadIdx.x == 0) update_length(p.length + b, p.ticket + (int64_t)b * p.stride, (int32_t)p.per, length + n);
+  const uint32_t from = to - mine, all = (uint32_t)__builtin_amdgcn_readlane((int)to, 63);
+  for (uint32_t item = blockIdx.x * waves + wave; item < all; item += gridDim.x * waves) {
+    const int b = __builtin_popcountll(__ballot(from <= item)) - 1;  // (the last one that begins there: it has tiles)
+    auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, b); };
+    append_tile<T, I8>(p, (uint32_t)b, item - of(from), of(tiles), (int)of((uint32_t)length), (int)of((uint32_t)n),
+                       lane);
+  }
+  __syncthreads();  // (the workgroup's waves have read the lengths)
+  if (wave != 0) return;
+  int drawn = 0;
+  if (lane == 0) drawn = __hip_atomic_fetch_add(p.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (__builtin_amdgcn_readfirstlane(drawn) != (int)gridDim.x - 1) return;
+  if (lane == 0) __hip_atomic_store(p.ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if ((uint32_t)lane < p.seqs) p.length[lane] = (int)min((int64_t)length + n, (int64_t)0x7fffffff);
+}
+
+enum AppendForm { kFew, kMany, kAll };
+
+// (Two workgroups of a tile per wave are to run on a CU: 128 registers.)
+template <typename T, bool I8, AppendForm F>
+__global__ __launch_bounds__(F == kFew ? 1024 : kAppendWaves * 64, 4) void window_append_kernel(AppendParams p) {
+  if constexpr (F == kAll) {
+    append_all<T, I8>(p);
+  } else {
+    const uint32_t b = blockIdx.x / p.per, part = blockIdx.x - b * p.per;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t waves = blockDim.x >> 6;
+    const int64_t length = max((int)__builtin_amdgcn_readfirstlane(p.length[b]), 0);
+    const int64_t n = new_tokens(p.lengths, b, p.T);
+    for (uint32_t item = part * waves + wave; item < p.items; item += p.per * waves) {
+      if constexpr (F == kFew) append_few<T, I8>(p, b, item, threadIdx.x & 63);
+      else append_tile<T, I8>(p, b, item, p.tiles, length, n, threadIdx.x & 63);
+    }
+    __syncthreads();  // (the workgroup's waves have read the length)
+    if (threadIdx.x == 0) update_length(p.length + b, p.ticket + (int64_t)b * p.stride, (int32_t)p.per, length + n);
+  }
 }
 
 struct KeepParams {
@@ -350,17 +393,22 @@ hipError_t launch_window_append(const gca_window& w, const void* k, const void* 
   // few tokens: as many waves per workgroup as go, so that one may do for a sequence and needs no ticket
   const uint32_t waves = few ? (p.items < 16 ? p.items : 16) : kAppendWaves;
   p.per = (p.items + waves - 1) / waves;
-  if (!few) {  // no more workgroups than run at once: every one takes a ticket (103 MB in 24 us, one per 8 tiles 34)
+  if (!few) {  // no more workgroups than run at once: every one takes a ticket (113 MB in 23 us, one per 8 tiles 33)
     const uint32_t most = 2 * (uint32_t)device_cus() / p.seqs;
     if (p.per > most) p.per = most > 1 ? most : 1;
   }
   p.ring = w.window > 0;
+  // a tile per wave and more: over all sequences' tiles, so that no workgroup is left with a long one while others are
+  // through (four prompts of up to 8,192 tokens: 30.6 us for 34.8; below that one ticket for all is 1 us more)
+  const bool all = !few && p.seqs > 1 && p.seqs <= 64 && p.items >= p.per * waves;
   const dim3 grid(p.seqs * p.per), block(waves * 64);
   auto run = [&](auto tag, auto i8) {
     using E = decltype(tag);
     constexpr bool I8 = decltype(i8)::value;
-    launch_kernel("window_append_kernel", few ? window_append_kernel<E, I8, true> : window_append_kernel<E, I8, false>,
-                  grid, block, 0, stream, p);
+    auto kernel = window_append_kernel<E, I8, kMany>;
+    if (few) kernel = window_append_kernel<E, I8, kFew>;
+    else if (all) kernel = window_append_kernel<E, I8, kAll>;
+    launch_kernel("window_append_kernel", kernel, grid, block, 0, stream, p);
   };
   if (w.dtype == GCA_BF16) w.format == GCA_INT8 ? run(__bf16{}, std::true_type{}) : run(__bf16{}, std::false_type{});
   else w.format == GCA_INT8 ? run(float{}, std::true_type{}) : run(float{}, std::false_type{});

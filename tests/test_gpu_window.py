@@ -206,6 +206,12 @@ APPEND = [
     (1, 2, 128, 0, 5, "bf16", "e4m3", [126], None),
     (1, 2, 128, 0, 5, "bf16", "int8", [128], None),
     (1, 16, 1024, 512, 700, "bf16", "e4m3", [900], None),                      # many workgroups
+    (5, 4, 256, 100, 100, "bf16", "e4m3", [0, 3, 64, 255, 9000], [100, 0, 1, 64, 99]),  # over all sequences' tiles
+    (5, 4, 256, 0, 100, "fp32", "int8", [0, 156, 157, 255, 9000], None),
+    (3, 4, 128, 64, 1000, "fp32", "e4m3", [1, 0, 63], [0, 0, 0]),
+    (64, 2, 192, 64, 190, "bf16", "int8", list(range(0, 640, 10)), list(range(-1, 191, 3))),
+    (3, 16, 1024, 512, 3000, "bf16", "e4m3", [0, 70, 1023], [3000, 1500, 17]),
+    (65, 2, 128, 64, 70, "bf16", "e4m3", list(range(65)), None),               # more sequences than lanes
 ]
 
 
