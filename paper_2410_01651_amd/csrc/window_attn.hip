@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
   // item = ((b Hkv + h) blocks + block) splits + split, unless the sequences' lengths have a say
   uint32_t b, h, blk, split, splits = p.splits, it;
-  uint32_t bare = 0;  // blocks from here on (of each head, cut head by head) have no tokens; 0: not this one's to write
+  int bare = -1;  // blocks from here on (of each head, cut head by head) have no tokens; -1: not this one's to write
   if (p.balance) {
     // A head's B blocks splits workgroups are dealt out by what its sequences have to do: one to each block that
     // has tokens, the others in proportion to the block's tiles.  Lane i: sequence i.
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       const uint32_t gh = scalar(blk / per);
       blk = gh * p.per_head + (blk - gh * per);
     }
-    if (i == 0) bare = per;
+    if (i == 0) bare = of(tok) > 0 ? (int)per : 0;
   } else {
     it = (uint32_t)xcd_swizzle(__builtin_amdgcn_workgroup_id_x(), (p.items + 7) / 8 * 8);
     if (it >= p.items) return;
@@ -263,8 +263,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
   };
 
   const int64_t row0 = (int64_t)(b * p.H + h * p.G) * p.T;
-  if (bare > 0) {  // (rows that nobody else gets to)
-    const uint32_t heads = p.per_head ? p.G : 1, from = bare * QB, rows = p.per_head ? p.T : p.M;
+  if (bare >= 0) {  // (rows that nobody else gets to)
+    const uint32_t heads = p.per_head ? p.G : 1, from = (uint32_t)bare * QB, rows = p.per_head ? p.T : p.M;
     for (uint32_t gh = 0; gh < heads; ++gh)
       for (uint32_t e = tid; from < rows && e < (rows - from) * 16; e += 64 * nw) {
         uint32_t g_, t_, m = from + (e >> 4);

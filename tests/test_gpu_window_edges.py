@@ -62,6 +62,36 @@ def test_attn_of_unequal_sequences(dev, gca, case):
     assert not w.ticket.any()
 
 
+@pytest.mark.parametrize("B,T,G,C,window,fmt", [
+    (3, 64, 8, 1024, 0, "int8"), (3, 33, 2, 1024, 0, "e4m3"), (3, 70, 3, 1024, 0, "e4m3"), (4, 1, 8, 1024, 0, "e4m3"), (4, 5, 8, 1024, 0, "int8"),
+    (5, 20, 3, 2048, 0, "e4m3"), (3, 130, 1, 1024, 0, "e4m3"), (2, 5, 3, 512, 0, "e4m3"), (3, 64, 8, 1024, 900, "int8"), (4, 9, 4, 1024, 500, "e4m3"),
+    (1, 64, 4, 4096, 0, "e4m3"), (70, 40, 2, 1024, 0, "e4m3"), (4, 64, 4, 512, 0, "e4m3"), (128, 64, 8, 128, 64, "e4m3")])
+def test_every_row_is_written(dev, gca, B, T, G, C, window, fmt):
+    """Whatever part of the rows has tokens (none of a sequence's, or of all, among them): out and lse hold NaN before."""
+    import torch
+    Hkv = 2
+    rng = np.random.default_rng(T + G)
+    w = gca.window(B, Hkv * G, C, window=window, Hkv=Hkv, format=fmt, device=dev)
+    g = tw._fill(w, 3, [int(x) for x in rng.integers(T, C + 1, B)])
+    q = torch.randn(B, Hkv * G, T, 64, generator=g, device=dev).bfloat16()
+    some = rng.integers(0, T + 1, B)
+    some[B // 2] = 0
+    few = np.full(B, T)
+    few[0] = 0
+    for n in (some, few, np.zeros(B), np.minimum(1, some), None):
+        lengths = None if n is None else torch.from_numpy(n.astype(np.int32)).to(dev)
+        for tree in ((False, True) if T <= 64 else (False,)):
+            par = torch.from_numpy(tw._tree(rng, B, T, "random")).to(dev) if tree else None
+            out = torch.full_like(q, float("nan"))
+            lse = torch.full(q.shape[:3], float("nan"), device=dev)
+            gca.window_attn(w, q, parents=par, lengths=lengths, out=out, lse=lse)
+            at = torch.arange(T, device=dev)[None, None] >= (T if n is None else lengths[:, None, None])
+            at = at.expand(B, Hkv * G, T)
+            assert (out[at] == 0).all() and (lse[at] == -float("inf")).all()
+            assert torch.isfinite(out[~at]).all() and torch.isfinite(lse[~at]).all()
+    assert not w.ticket.any()
+
+
 @pytest.mark.parametrize("dtype,fmt,B,T,G", [("bf16", "e4m3", 2, 9, 1), ("fp32", "int8", 2, 9, 1), ("bf16", "int8", 2, 9, 4),
                                               ("bf16", "e4m3", 16, 64, 4), ("fp32", "e4m3", 2, 33, 2), ("bf16", "e4m3", 1, 1, 1)])
 def test_odd_values_that_a_row_does_not_see(dev, gca, dtype, fmt, B, T, G):
