@@ -7,7 +7,7 @@
 // row's largest magnitude is a reduction over 8 lanes and the values' tile is byte blocks turned in
 // registers.  A tile that new tokens fill only in part (a single token's, a prompt's first and last)
 // writes its own rows and no others.  Few tokens are taken eight to a wave instead, a row for eight lanes, and are
-// read before the length that says where they go is there: 64 sequences' single tokens of 16 heads 5.0 us for 6.0.
+// read before the length that says where they go is there: 64 sequences' single tokens of 16 heads 5.0 us for 9.7.
 // Bound: few tokens by the trips to memory; many by HBM, at 2 B Hkv T (64 (e + 1) + 4) bytes: four prompts of
 // up to 8,192 tokens, 16 heads, 113 MB in 22.7 us, 5.0 TB/s, as a large copy, where the last cache still has
 // what was just computed, and 121 MB in 30.6 us, 3.9 TB/s, where it has not.  (Loads that leave that cache alone:
@@ -26,7 +26,9 @@ namespace gca {
 namespace {
 
 constexpr int kAppendWaves = 8;
-constexpr int64_t kFewTokens = 32;  // up to four eights: half of a tile's rows
+// Eight tokens to a wave / a tile to a wave: 64 sequences, 16 heads, 25 tokens 6.3 / 11.5 us, 64 tokens 10.4 / 13.5, 128
+// tokens 16.6 / 16.7, 512 tokens 56 / 38; 4 sequences, 8 heads, 128 tokens 4.2 / 6.1.
+constexpr int64_t kFewTokens = 128;
 constexpr int kRingTile = kS * kD;  // bytes of a tile's keys or values
 
 struct AppendParams {

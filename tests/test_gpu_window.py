@@ -212,6 +212,12 @@ APPEND = [
     (64, 2, 192, 64, 190, "bf16", "int8", list(range(0, 640, 10)), list(range(-1, 191, 3))),
     (3, 16, 1024, 512, 3000, "bf16", "e4m3", [0, 70, 1023], [3000, 1500, 17]),
     (65, 2, 128, 64, 70, "bf16", "e4m3", list(range(65)), None),               # more sequences than lanes
+    (65, 2, 128, 64, 140, "bf16", "e4m3", list(range(65)), None),
+    (5, 4, 256, 100, 140, "bf16", "e4m3", [0, 3, 64, 255, 9000], [140, 0, 1, 64, 99]),
+    (5, 4, 256, 0, 150, "fp32", "int8", [0, 106, 107, 255, 9000], None),
+    (3, 2, 192, 64, 129, "bf16", "e4m3", [0, 5, 191], [129, 0, 33]),
+    (2, 3, 128, 100, 128, "bf16", "int8", [127, 1000001], None),
+    (1, 2, 64, 64, 128, "fp32", "e4m3", [3], None),                            # twice what the ring holds
 ]
 
 
