@@ -389,7 +389,7 @@ typedef struct {
   int32_t d;
   int64_t capacity;     /* rows per sequence */
   int32_t window;       /* tokens that a row sees, itself included; 0: all */
-  float attn_scale;     /* multiplies <q, k> */
+  float attn_scale;     /* multiplies <q, k>; 0, or at least 2^-64 in magnitude */
   int32_t off_by_one;   /* 1: the softmax's denominator is 1 + its sum, as in gca_problem */
   int32_t dtype;        /* gca_dtype of q, k, v, out */
   int32_t format;       /* gca_format of the kept numbers */

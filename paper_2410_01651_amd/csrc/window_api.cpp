@@ -36,6 +36,9 @@ gca_status check_window(const gca_window* w) {
   if (w->off_by_one != 0 && w->off_by_one != 1) return fail(GCA_ERR_INVALID, "off_by_one must be 0 or 1");
   if (w->flags != 0) return fail(GCA_ERR_INVALID, "unknown flag bits");
   if (!std::isfinite(w->attn_scale)) return fail(GCA_ERR_INVALID, "scales must be finite");
+  // (biases are taken in units of a score before its scale)
+  if (w->attn_scale != 0.f && std::fabs(w->attn_scale) < 0x1p-64f)
+    return fail(GCA_ERR_UNSUPPORTED, "attn_scale must be 0 or at least 2^-64");
   if ((int64_t)w->B * w->H > kMaxItems / 16) return fail(GCA_ERR_UNSUPPORTED, "window too large for one launch");
   return GCA_OK;
 }

@@ -5,9 +5,9 @@
 // kept transposed per 64 rows.  One wave per 64 positions that share a tile of rows, and per keys or
 // values: lane (rg, cg) = (l / 8, l % 8) holds the 8 x 8 block of rows 8 rg .. and columns 8 cg .., so that a
 // row's largest magnitude is a reduction over 8 lanes and the values' tile is byte blocks turned in
-// registers.  A tile that new tokens fill only in part (a single token's, a prompt's first and last)
+// registers.  A tile that new tokens fill only in part (a prompt's first and last)
 // writes its own rows and no others.  Few tokens are taken eight to a wave instead, a row for eight lanes, and are
-// read before the length that says where they go is there: 64 sequences' single tokens of 16 heads 5.0 us for 9.7.
+// read before the length that says where they go is there: eight tokens of 64 sequences, 16 heads, 5.0 us for 9.7.
 // Bound: few tokens by the trips to memory; many by HBM, at 2 B Hkv T (64 (e + 1) + 4) bytes: four prompts of
 // up to 8,192 tokens, 16 heads, 113 MB in 22.7 us, 5.0 TB/s, as a large copy, where the last cache still has
 // what was just computed, and 121 MB in 30.6 us, 3.9 TB/s, where it has not.  (Loads that leave that cache alone:

@@ -26,7 +26,7 @@
 // tokens, 8 cached heads for 32: 76 us (411 MB, 5.4 TB/s).  Many rows (prompts): instruction issue, of which the
 // softmax has most: a tile of 64 x 64 takes 610 vector instructions beside its 32 MFMA.  8,192 tokens of 4
 // sequences, 16 heads, a window of 512: 125 us, vector pipes busy 68 %, MFMA 24 %.  A tree of 25 nodes over 8 cached heads for 32 heads, 16
-// sequences of up to 7,777 tokens: 40 us; four blocks of 32 rows unpack each tile, and vector pipes are busy 33 %.
+// sequences of up to 7,777 tokens: 41 us; four blocks of 32 rows unpack each tile, and vector pipes are busy 33 %.
 // One sequence's token of 8 heads over 512: 6 us, the trips to memory (length, tile, parts) one after the other.
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
@@ -809,7 +809,7 @@ WindowAttnPlan window_attn_plan(const gca_window& w, int64_t T) {
 
 // Where every row sees its sequence's all, some sequences may have far more to do than others: their blocks get
 // more workgroups.  The tree of 25 nodes over 16 sequences of 1 to 7,777 tokens: 54 us with as many for each,
-// 40 so; of equal lengths 33 either way.  (In workgroups of two waves 38, but of equal lengths 38.)
+// 41 so; of equal lengths with the same sum 33 either way.  (In workgroups of two waves 38, but of equal ones 38.)
 namespace {
 constexpr int kBalanceWaves = 4;  // per workgroup at least: fewer, and there are several rounds of them anyway
 bool may_balance(const gca_window& w) { return w.window == 0 && w.B > 1 && w.B <= 64 && w.capacity >= 1024; }

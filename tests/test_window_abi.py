@@ -73,7 +73,8 @@ def test_struct_layout(gca):
     ("capacity", 0, "INVALID"), ("capacity", 100, "UNSUPPORTED"), ("capacity", (1 << 24) + 64, "UNSUPPORTED"),
     ("window", -1, "INVALID"), ("window", 1025, "INVALID"), ("dtype", 2, "INVALID"), ("format", 2, "INVALID"),
     ("format", -1, "INVALID"), ("off_by_one", 2, "INVALID"), ("flags", 1, "INVALID"), ("attn_scale", math.nan, "INVALID"),
-    ("attn_scale", math.inf, "INVALID"), ("B", 1 << 20, "UNSUPPORTED"),
+    ("attn_scale", math.inf, "INVALID"), ("attn_scale", 1e-40, "UNSUPPORTED"), ("attn_scale", -(2.0**-65), "UNSUPPORTED"),
+    ("B", 1 << 20, "UNSUPPORTED"),
 ])
 def test_malformed_window_is_refused(gca, field, value, status):
     w = _window(gca, **{field: value})
