@@ -16,7 +16,8 @@
 // Bound by HBM, the last node's p (and q, where it was rejected from), or, for few sequences, by
 // the trips to memory.  64 chains of 8, 100,000 tokens: 12 us of walk and sums (51 MB, 4.3 TB/s) and 4 of the draw;
 // one chain of 5, 32,000 tokens: 4.8 and 3.9.  In one launch, a workgroup of 1,024 threads per sequence: 12.8 us for
-// that chain (8.2 for 2,000 tokens), as one CU reads its rows, and for 1,024 of them 53.6 for 30 and 11.  All first children's tests at once: 32 trees of up to 25 nodes 8.4 us for 9.9.
+// that chain (8.2 for 2,000 tokens), as one CU reads its rows, and for 1,024 of them 53.6 for 30 and 11.  All first
+// children's tests at once: 32 trees of up to 25 nodes 8.4 us for 9.9.
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
 #include "window_plan.hpp"

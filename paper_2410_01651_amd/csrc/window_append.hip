@@ -315,7 +315,7 @@ struct KeepParams {
   int ring;
 };
 
-constexpr int kKeepWaves = 4;   // (16: 18.7 us for 6.9, as many waves wait for the one that draws the ticket)
+constexpr int kKeepWaves = 4;   // (16: 18.7 us for 6.9)
 constexpr int kKeepTokens = 8;  // at a time
 
 // One wave per (sequence, cached head).
@@ -395,7 +395,7 @@ hipError_t launch_window_append(const gca_window& w, const void* k, const void* 
   // few tokens: as many waves per workgroup as go, so that one may do for a sequence and needs no ticket
   const uint32_t waves = few ? (p.items < 16 ? p.items : 16) : kAppendWaves;
   p.per = (p.items + waves - 1) / waves;
-  if (!few) {  // no more workgroups than run at once: every one takes a ticket (113 MB in 23 us, one per 8 tiles 33)
+  if (!few) {  // no more workgroups than run at once: every one takes a ticket (a workgroup per 8 tiles: 34 us for 24)
     const uint32_t most = 2 * (uint32_t)device_cus() / p.seqs;
     if (p.per > most) p.per = most > 1 ? most : 1;
   }
