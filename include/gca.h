@@ -419,7 +419,8 @@ gca_status gca_window_append(const gca_window* w, const void* k, const void* v, 
  * with scores  attn_scale <q, k> + slopes[h] (position of the key - position of the row),
  * one softmax over all of them, and out = softmax V.  Rows from n_b on, and rows that see nothing, get out = 0
  * and lse = -inf.  What a row does not see has no effect on it, whatever it is (a value's number that is NaN,
- * which gca_window_append never stores, in a row that others see aside).
+ * which gca_window_append never stores, in a row that others see aside), but for the roundings below: they go by
+ * value scales that other rows of its block see.
  *   q       [B, H, T, d] dtype
  *   parents [B, T]       int32  of each node; entries outside 0 .. i - 1 make node i a root.  Needs
  *                               T <= 64.  NULL: a chain, of any T
@@ -431,7 +432,7 @@ gca_status gca_window_append(const gca_window* w, const void* k, const void* v, 
  * longer prompt comes in pieces; GCA_ERR_INVALID).  Products of q with the kept numbers are exact and summed
  * in fp32.  Probabilities relative to the row's largest so far, with their value scale in them, are rounded to
  * fp16 (fp32 tensors: to two fp16 terms): by 2^-11 (2^-22) of themselves, or, where they are so small, by up to a
- * 2^-39th of the largest value scale that the row's block of rows has met.  (Blocks of 64 rows, for
+ * 2^-39th of the largest value scale that a row of the row's block sees.  (Blocks of 64 rows, for
  * GCA_E4M3 and bf16 where there are enough to fill the chip, round the probabilities alone, by 2^-11 or 2^-40, and
  * hold values in fp16, exactly, or, where they are so small, to a 2^-30th of that scale.)
  * Requires w->k, v, k_scale, v_scale, length, ticket.  Workspace: gca_window_workspace_size(w, T)

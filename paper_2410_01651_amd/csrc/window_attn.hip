@@ -7,9 +7,10 @@
 // Every e4m3 number and every int8 is exact in bf16 and in fp16.  An e4m3 key takes its scale (a power of
 // two) along in the conversion; int8 scores are multiplied by theirs.  So q N^T is a product of exact
 // operands with fp32 sums (fp32 queries: three bf16 terms, 24 bits), and P nu / u meets M in fp16,
-// 11 bits (fp32 tensors: two fp16 terms, 22 bits), u being a power of two by the largest nu that the block of
-// rows has met so far: P <= 1, so fp16 holds the product, and when a tile brings a larger nu what was
-// summed is rescaled with the same factor that a new maximum brings.
+// 11 bits (fp32 tensors: two fp16 terms, 22 bits), u being a power of two by the largest nu that a row of
+// the block has seen so far: P <= 1, so fp16 holds the product, and when a tile brings a larger nu what was
+// summed is rescaled with the same factor that a new maximum brings.  (Tokens that none of the block's rows sees, behind
+// them, before their windows or on other branches, have no say in u: it may be any number that they bring.)
 //
 // Layout.  As in the chunk cache's attention: S^T = N Q^T and O^T = M^T P^T on MFMA tiles of W x W, lane
 // l = W g + c having query row c as its column, the rows of N in the order that makes a lane's
@@ -73,6 +74,21 @@ struct WindowParams {
 // (By its bits, and where the compiler does not know them for a float's: to this file's comparisons of floats
 // NaN may be anything.)
 __device__ __forceinline__ bool is_zero(float x) { return opaque((int)__float_as_uint(x)) << 1 == 0; }
+
+// x of the W lanes of a group joined by f, in every lane of it.
+template <int W, typename F>
+__device__ __forceinline__ uint32_t fold_rows(uint32_t x, F f) {
+  x = f(x, dpp<kDppXor1>(x));
+  x = f(x, dpp<kDppXor2>(x));
+  x = f(x, dpp<kDppRor4>(x));
+  x = f(x, dpp<kDppRor8>(x));
+  if constexpr (W == 32) {
+    uint32_t a, b;
+    pair16(x, a, b);
+    x = f(a, b);
+  }
+  return x;
+}
 
 // out = sum_w exp2(m_w - m) o_w / (sum_w exp2(m_w - m) l_w), and the row's log-sum-exp.
 struct Joined {
@@ -312,20 +328,42 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * i, (int)(uint32_t)(up >> 32));
     return (uint64_t)hi << 32 | lo;
   };
+  // of a node's ancestors and itself those that it sees: less than `window` levels up
+  auto near = [&](uint64_t sees, int deep) {
+    if (p.window)
+      for (int x = deep - p.window; x >= 0; --x) sees &= sees - 1;
+    return sees;
+  };
+  uint32_t seen_lo = 0, seen_hi = 0, dlow = kTreeNodes;  // of a tree: the nodes that the block's rows see, and their least depth
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     uint32_t gh, t;
     place(min((uint32_t)(c * W + col), nrows - 1), gh, t);
     row[c] = gh * p.T + t;
     depth[c] = (int)t;
-    if constexpr (TREE) depth[c] = __builtin_popcountll(above((int)t)) - 1;
+    if constexpr (TREE) {
+      const uint64_t sees = above((int)t);
+      depth[c] = __builtin_popcountll(sees) - 1;
+      const uint64_t mine = (int)t < n ? near(sees, depth[c]) : 0ull;
+      seen_lo |= (uint32_t)mine;
+      seen_hi |= (uint32_t)(mine >> 32);
+      dlow = min(dlow, (int)t < n ? (uint32_t)depth[c] : (uint32_t)kTreeNodes);
+    }
     slope[c] = p.slopes ? p.slopes[h * p.G + gh] * p.unscale : 0.f;
+  }
+  uint64_t nodes = 0;
+  if constexpr (TREE) {
+    seen_lo = fold_rows<W>(seen_lo, [](uint32_t x, uint32_t y) { return x | y; });
+    seen_hi = fold_rows<W>(seen_hi, [](uint32_t x, uint32_t y) { return x | y; });
+    dlow = fold_rows<W>(dlow, [](uint32_t x, uint32_t y) { return min(x, y); });
+    nodes = (uint64_t)scalar(seen_hi) << 32 | scalar(seen_lo);
+    dlow = scalar(dlow);
   }
 
   // ---- tiles of 64 positions that the rows see: [t0, t1)
-  const int dmin = TREE ? 0 : (int)tmin, dmax = TREE ? kTreeNodes - 1 : (int)tmax;
+  const int dmin = TREE ? (int)dlow : (int)tmin, dmax = TREE ? kTreeNodes - 1 : (int)tmax;
   const int first = p.window ? max(base + dmin - p.window + 1, 0) : 0;
-  const int last = TREE ? length - 1 : min(base + (int)tmax, length - 1);  // position
+  const int last = base + min((int)tmax, n - 1);  // position (a node sees none behind its own)
   const int t0 = first >> 6;
   int t1 = (last >> 6) + 1;
   if (!p.ring) t1 = min(t1, (int)p.ring_tiles);
@@ -417,9 +455,13 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     const bool more = tn >= t0;
     const uint32_t sn = more ? slot(tn) : 0;
 
-    // scales, those of values over u: tokens that nobody sees have none
-    const int from = first - p0, to = length - p0;  // what may be seen of the tile
-    const bool here = lane >= from && lane < to;
+    // scales, those of values over u: tokens that no row of the block sees have none
+    const int from = first - p0, to = length - p0;  // what there is of the tile
+    bool here = lane >= from && lane <= last - p0;
+    if (TREE && p0 + kS > base) {
+      const int node = p0 + lane - base;
+      here = here && (node < 0 || (nodes >> (node & 63) & 1) != 0);
+    }
     const float nu = here ? vsc : 0.f;
     int up_by = 0;  // octaves that u grows by
     if (__ballot(nu > limit) != 0) {
@@ -490,11 +532,10 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       if (TREE && masked) {
         const int off = base - p0;  // the first new token
         bits = off >= 64 ? ~0ull : off > 0 ? (1ull << off) - 1 : 0ull;
-        uint64_t sees = above(token(c));
-        if (p.window) {  // without ancestors `window` levels up or more
+        const uint64_t sees = near(above(token(c)), depth[c]);
+        if (p.window) {
           const int l = lo + 16 * g;
           bits = l < 64 ? bits & (~0ull << l) : 0ull;
-          for (int x = depth[c] - p.window; x >= 0; --x) sees &= sees - 1;
         }
         if (off < 64) bits |= off >= 0 ? sees << off : off > -64 ? sees >> -off : 0ull;
         if (to < 64) bits &= to > 0 ? (1ull << to) - 1 : 0ull;
