@@ -417,8 +417,9 @@ gca_status gca_window_append(const gca_window* w, const void* k, const void* v, 
  *   - the positions p < base with p > base + depth(i) - window,
  *   - itself and its ancestors (a chain: the new tokens before it) less than `window` levels above,
  * with scores  attn_scale <q, k> + slopes[h] (position of the key - position of the row),
- * one softmax over all of them, and out = softmax V.  Rows from n_b on, and rows that see nothing, get out = 0
- * and lse = -inf.  What a row does not see has no effect on it, whatever it is (a value's number that is NaN,
+ * one softmax over all of them, and out = softmax V.  Rows from n_b on, rows that see nothing and rows whose scores
+ * are all -inf get out = 0 and lse = -inf.  NaN in a row's query or in the scales of a token that it sees comes
+ * out as NaN, and so does an infinity in its query that leaves a score above -inf.  What a row does not see has no effect on it, whatever it is (a value's number that is NaN,
  * which gca_window_append never stores, in a row that others see aside), but for the roundings below: they go by
  * value scales that other rows of its block see.
  *   q       [B, H, T, d] dtype

@@ -71,10 +71,6 @@ struct WindowParams {
   int off_by_one;
 };
 
-// (By its bits, and where the compiler does not know them for a float's: to this file's comparisons of floats
-// NaN may be anything.)
-__device__ __forceinline__ bool is_zero(float x) { return opaque((int)__float_as_uint(x)) << 1 == 0; }
-
 // x of the W lanes of a group joined by f, in every lane of it.
 template <int W, typename F>
 __device__ __forceinline__ uint32_t fold_rows(uint32_t x, F f) {
@@ -142,16 +138,16 @@ __device__ __forceinline__ void join_rows_by(const WindowParams& p, uint32_t fir
     top = now;
 #pragma unroll
     for (uint32_t s = 0; s < kAhead; ++s) {
-      if (s0 + s >= n || is_zero(ml[s][1])) continue;
+      if (s0 + s >= n || ml[s][1] == 0.f) continue;
       const float f = __builtin_amdgcn_exp2f(ml[s][0] - top);
       l = fmaf(ml[s][1], f, l);
       acc += f32x4{a[s][0], a[s][1], c[s][0], c[s][1]} * f;
     }
   }
   const Joined j = finish(top, l, p.off_by_one);
-  const float f = is_zero(l) ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
+  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
   store4(reinterpret_cast<T*>(p.out) + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
-  if (p.lse && x == 0) p.lse[r] = is_zero(l) ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+  if (p.lse && x == 0) p.lse[r] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
 }
 
 template <typename T, int QB>
@@ -161,8 +157,6 @@ __device__ __forceinline__ void join_rows(const WindowParams& p, uint32_t first,
   else join_rows_by<T, QB, 8>(p, first, n, m, x, r);
 }
 
-// (Indices by builtin: what is behind threadIdx and its like does not inline under this file's
-// floating point flags and would be called.)
 // T: type of the queries; W: MFMA tile; NC: column blocks of W query rows; TREE: the new tokens are a tree.
 template <typename T, bool I8, int W, int NC, bool TREE>
 __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowParams p) {
@@ -700,7 +694,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       const uint32_t m = c * W + col;
       if (m >= nrows) continue;
       const Joined j = finish(mx[c], sum[c], p.off_by_one);
-      const bool none = token(c) >= n || is_zero(sum[c]);
+      const bool none = token(c) >= n || sum[c] == 0.f;
       // (off by one: the row's own scale between its maximum and the denominator's)
       const float f = none ? 0.f : __builtin_amdgcn_exp2f(mx[c] - j.m) / j.l;
       const int64_t r = row_of(m);
@@ -749,7 +743,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     float l = 0.f;
     for (uint32_t y = 0; y < nw; ++y) {
       const float ly = ml[2 * (y * nrows + m) + 1];
-      if (is_zero(ly)) continue;
+      if (ly == 0.f) continue;
       const float f = __builtin_amdgcn_exp2f(ml[2 * (y * nrows + m)] - top);
       l = fmaf(ly, f, l);
       const f32x4 oy = *reinterpret_cast<const f32x4*>(part + (y * nrows + m) * kD + 4 * (x ^ (m & 15)));
@@ -762,11 +756,11 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
       if (x == 0) put2(p.part_ml + at * 2, top, l);
     } else {
       const Joined j = finish(top, l, p.off_by_one);
-      const float f = is_zero(l) ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
+      const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - j.m) / j.l;
       const int64_t r = row_of(m);
       store4(out0 + r * kD + 4 * x, acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f);
       if (p.lse && x == 0)
-        p.lse[row0 + r] = is_zero(l) ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
+        p.lse[row0 + r] = l == 0.f ? -INFINITY : (j.m + __builtin_amdgcn_logf(j.l)) * kLn2;
     }
   }
   if (splits == 1 || !p.ticket) return;
