@@ -205,6 +205,18 @@ def _check(status: int) -> None:
         raise GcaError(status, f"{L.gca_status_string(status).decode()}: {L.gca_last_error().decode()}")
 
 
+_WHOLE = (ctypes.c_int32, ctypes.c_int64)
+
+
+def _sized(struct, **fields):
+    """A struct of these fields, the sizes among them as they are given: ctypes would take them modulo a power of
+    two, and one that does not fit would become another."""
+    for name, kind in struct._fields_:
+        if name in fields and kind in _WHOLE and kind(fields[name]).value != fields[name]:
+            raise ValueError(f"{name} = {fields[name]} does not fit")
+    return struct(**fields)
+
+
 def problem(B, H, n_chunks, topk, D=None, Hr=1, d=64, S=64, score_scale=None, attn_scale=None,
             off_by_one=False, dtype="bf16", mode="causal", flags=0, gumbel_seed=None,
             lmk_row=False) -> Problem:
@@ -216,8 +228,8 @@ def problem(B, H, n_chunks, topk, D=None, Hr=1, d=64, S=64, score_scale=None, at
         flags |= FLAG_GUMBEL
     if lmk_row:
         flags |= FLAG_LMK_ROW
-    return Problem(
-        B=B, H=H, d=d, S=S, n_chunks=n_chunks, topk=topk, Hr=Hr, D=D,
+    return _sized(
+        Problem, B=B, H=H, d=d, S=S, n_chunks=n_chunks, topk=topk, Hr=Hr, D=D,
         score_scale=1.0 / math.sqrt(D) if score_scale is None else score_scale,
         attn_scale=1.0 / math.sqrt(d) if attn_scale is None else attn_scale,
         off_by_one=int(bool(off_by_one)),
@@ -521,13 +533,14 @@ def cache(B, H, capacity, topk, Hkv=None, Hr=1, D=None, score_scale=None, attn_s
     types = dict(k=num, v=num, k_scale=torch.float32, v_scale=torch.float32, lmk=elem, tokens=torch.int32,
                  mass=torch.float32, number=torch.int32, next=torch.int32)
     sh = cache_shapes(B, Hkv, capacity, Hr, D)
-    given, device = _members(sh, types, tensors, device, "cache")
-    struct = CacheStruct(
-        B=B, H=H, Hkv=Hkv, Hr=Hr, d=64, S=64, capacity=capacity, topk=topk, D=D,
+    struct = _sized(
+        CacheStruct, B=B, H=H, Hkv=Hkv, Hr=Hr, d=64, S=64, capacity=capacity, topk=topk, D=D,
         score_scale=1.0 / math.sqrt(D) if score_scale is None else score_scale,
         attn_scale=0.125 if attn_scale is None else attn_scale, off_by_one=int(bool(off_by_one)),
-        dtype=GCA_BF16 if dtype == "bf16" else GCA_FP32, format=GCA_E4M3 if format == "e4m3" else GCA_INT8, flags=0,
-        **{name: given[name].data_ptr() for name in sh})
+        dtype=GCA_BF16 if dtype == "bf16" else GCA_FP32, format=GCA_E4M3 if format == "e4m3" else GCA_INT8, flags=0)
+    given, device = _members(sh, types, tensors, device, "cache")
+    for name in sh:
+        setattr(struct, name, given[name].data_ptr())
     return Cache(struct, given, device, device.index)
 
 
@@ -741,8 +754,8 @@ def window(B, H, capacity, window=0, Hkv=None, attn_scale=None, off_by_one=False
     Hkv = H if Hkv is None else Hkv
     num = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}[format]
     types = dict(k=num, v=num, k_scale=torch.float32, v_scale=torch.float32, length=torch.int32, ticket=torch.int32)
-    struct = WindowStruct(
-        B=B, H=H, Hkv=Hkv, d=64, capacity=capacity, window=window, attn_scale=0.125 if attn_scale is None else attn_scale,
+    struct = _sized(
+        WindowStruct, B=B, H=H, Hkv=Hkv, d=64, capacity=capacity, window=window, attn_scale=0.125 if attn_scale is None else attn_scale,
         off_by_one=int(bool(off_by_one)), dtype={"bf16": GCA_BF16, "fp32": GCA_FP32}[dtype],
         format=GCA_E4M3 if format == "e4m3" else GCA_INT8, flags=0)
     sh = window_shapes(B, H, Hkv, capacity)
@@ -809,6 +822,8 @@ def window_keep(w: Window, T, path, lengths=None, stream=None):
     if path.dim() != 2:
         raise ValueError("path must have shape (B, n)")
     n = path.shape[1]
+    if T >> 63 not in (0, -1):
+        raise ValueError(f"T = {T} does not fit")
     with _at(w, stream) as st:
         _check(lib().gca_window_keep(w.ref, _cache_ptr(w, path, "path", i32, (B, n)), n,
                                      _cache_ptr(w, lengths, "lengths", i32, (B,)), T, st))
