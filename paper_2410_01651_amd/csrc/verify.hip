@@ -52,7 +52,7 @@ struct VerifyParams {
   int32_t* next;
   Walk* walk;      // [B]
   uint64_t* sums;   // [B][slices][waves]
-  uint32_t B, T, slices;
+  uint32_t T, slices;
   uint32_t V, per;  // entries in all, and per wave of a slice (a multiple of 4)
 };
 
@@ -475,7 +475,6 @@ hipError_t launch_verify(int64_t B, int64_t T, int64_t V, const float* p, const 
   k.next = next;
   k.walk = static_cast<Walk*>(ws);
   k.sums = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + align256((size_t)B * sizeof(Walk)));
-  k.B = (uint32_t)B;
   k.T = (uint32_t)T;
   k.slices = (uint32_t)a.slices;
   k.V = (uint32_t)V;

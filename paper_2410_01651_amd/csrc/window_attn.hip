@@ -777,25 +777,20 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void window_attn_kernel(WindowPa
     join_rows<T, QB>(p, it - split, splits, e >> 4, e & 15, row0 + row_of(e >> 4));
 }
 
-// The same in a launch of its own, where a window has no tickets for so many row blocks (cut head by head, then): 16
-// threads per row.
+// The same in a launch of its own, where a window has no tickets for so many row blocks: more than two per
+// head, which only rows cut head by head come to (p.per_head > 0; as lists a group's rows make at most a block per
+// head).  16 threads per row.
 template <typename T, int QB>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowParams p) {
   const uint32_t e = __builtin_amdgcn_workgroup_id_x() * 256 + __builtin_amdgcn_workitem_id_x();
   const uint32_t x = e & 15, m = (e >> 4) % QB, bb = (e >> 4) / QB;
   const uint32_t bh = bb / p.blocks, blk = bb - bh * p.blocks;
   if (bb >= p.items / p.splits) return;
-  uint32_t at0, nrows;
-  if (p.per_head) {
-    const uint32_t gh = blk / p.per_head, tmin = (blk - gh * p.per_head) * QB;
-    nrows = min((uint32_t)QB, p.T - tmin);
-    at0 = gh * p.T + tmin;
-  } else {
-    at0 = blk * QB;
-    nrows = min((uint32_t)QB, p.M - at0);
-  }
+  const uint32_t gh = blk / p.per_head, tmin = (blk - gh * p.per_head) * QB;
   const uint32_t b = bh / p.Hkv, h = bh - b * p.Hkv;
-  if (m < nrows) join_rows<T, QB>(p, bb * p.splits, p.splits, m, x, (int64_t)(b * p.H + h * p.G) * p.T + at0 + m);
+  if (m < min((uint32_t)QB, p.T - tmin))
+    join_rows<T, QB>(p, bb * p.splits, p.splits, m, x,
+                     (int64_t)(b * p.H + h * p.G) * p.T + gh * p.T + tmin + m);
 }
 
 }  // namespace
