@@ -378,7 +378,8 @@ size_t gca_cache_workspace_size(const gca_cache* c, int op, int64_t n);
  * Numbers.  As in the chunk cache, but with one scale per token and cached head for its 64
  * keys, and one for its 64 values: the least power of two (at least 2^-126) that brings the largest
  * finite magnitude to at most 448 (GCA_E4M3), or that magnitude (at least 2^-100) over 127
- * (GCA_INT8).  Infinities are stored as the largest number; a token with a NaN among its keys
+ * (GCA_INT8; an entry is multiplied in fp32 by 127 times the magnitude's reciprocal, and rounded to the nearest, ties
+ * to even).  Infinities are stored as the largest number; a token with a NaN among its keys
  * (values) has the scale NaN for its keys (values).
  *
  * B sequences; H query heads share Hkv cached heads, as in gca_cache.  Supported: d == 64, H a

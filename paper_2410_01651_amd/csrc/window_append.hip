@@ -92,7 +92,9 @@ __device__ __forceinline__ float numbers_of(const Row8<T>& x, uint32_t top, bool
   if constexpr (I8) {
     const float amax = fmaxf(__uint_as_float(top), 0x1p-100f);
     scale = amax / 127.f;
-    const float inv = 127.f / amax;  // |x| inv <= 127 (1 + 2 roundings): 127 at most once rounded
+    // As the chunk cache forms it, so that the same tokens are the same numbers in both (ties are common among bf16
+    // entries, and go by the factor's last bit).  |x| inv <= 127 (1 + 2^-21): 127 at most once rounded
+    const float inv = (1.f / amax) * 127.f;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       uint32_t o = 0;
