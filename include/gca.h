@@ -373,7 +373,8 @@ size_t gca_cache_workspace_size(const gca_cache* c, int op, int64_t n);
  *
  * length[b] counts the tokens of sequence b, the newest included; position p is in row
  * p mod capacity (window > 0: a ring), or in row p if p < capacity (window = 0: all tokens are
- * seen; those past the capacity are counted but neither kept nor seen).
+ * seen; those past the capacity are counted but neither kept nor seen).  Sequences of up to 2^30
+ * tokens.
  *
  * Numbers.  As in the chunk cache, but with one scale per token and cached head for its 64
  * keys, and one for its 64 values: the least power of two (at least 2^-126) that brings the largest
@@ -384,7 +385,7 @@ size_t gca_cache_workspace_size(const gca_cache* c, int op, int64_t n);
  *
  * B sequences; H query heads share Hkv cached heads, as in gca_cache.  Supported: d == 64, H a
  * multiple of Hkv, B H < 2^19, capacity a multiple of 64 up to 2^24, window 0 .. capacity, and
- * calls of T tokens with B H T up to 2^26. */
+ * calls of T tokens with T up to 16 floor((2^23 - 8) / (B H)), so B H T up to 2^26 at least. */
 typedef struct {
   int32_t B, H, Hkv;
   int32_t d;
@@ -431,12 +432,15 @@ gca_status gca_window_append(const gca_window* w, const void* k, const void* v, 
  *   out     [B, H, T, d] dtype  output
  *   lse     [B, H, T]    fp32   output: log of each row's softmax denominator; may be NULL
  * In a ring, a row's window has to outlast the new tokens: window + T - 1 <= capacity (a
- * longer prompt comes in pieces; GCA_ERR_INVALID).  Products of q with the kept numbers are exact and summed
+ * longer prompt comes in pieces; GCA_ERR_INVALID).  Products of q with the kept numbers are exact (GCA_E4M3: with
+ * scales from 2^-117 up, below which keys times their scale are bf16 numbers without all their bits) and summed
  * in fp32.  Probabilities relative to the row's largest so far, with their value scale in them, are rounded to
  * fp16 (fp32 tensors: to two fp16 terms): by 2^-11 (2^-22) of themselves, or, where they are so small, by up to a
  * 2^-39th of the largest value scale that a row of the row's block sees.  (Blocks of 64 rows, for
  * GCA_E4M3 and bf16 where there are enough to fill the chip, round the probabilities alone, by 2^-11 or 2^-40, and
- * hold values in fp16, exactly, or, where they are so small, to a 2^-30th of that scale.)
+ * hold values in fp16, exactly, or, where they are so small, to a 2^-30th of that scale.)  The same call on the same
+ * state gives the same bits.  How the work is cut, and with it the order of sums, goes by the call's sizes and, with
+ * window = 0, by all sequences' lengths: a sequence in another batch keeps to these roundings, but not to the bit.
  * Requires w->k, v, k_scale, v_scale, length, ticket.  Workspace: gca_window_workspace_size(w, T)
  * bytes, 256-byte aligned. */
 gca_status gca_window_attn(const gca_window* w, const void* q, const int32_t* parents, const int32_t* lengths,
@@ -470,7 +474,8 @@ size_t gca_window_workspace_size(const gca_window* w, int64_t T);
  * When no child is left, the next token is drawn from r: the first x whose partial sum r[0] + .. + r[x]
  * exceeds u[0] sum r.  If r is zero everywhere, from p[a]; if that is too, next = -1.  Probabilities count
  * as 0 where they are negative or NaN and as 1 above 1.  Products and differences are in fp64, and sums are of
- * r to the nearest 2^-44, exactly: they do not depend on their order.
+ * r to the nearest 2^-44, exactly: they do not depend on their order.  (With q, the R-th rejected child of a node that
+ * has a sibling left takes a pass over p[a] and q[a] of about R steps per entry: trees of a few siblings are meant.)
  *   p, q    [B, T, V] fp32 (q may be NULL)
  *   tokens  [B, T]    int32  drafted tokens; one outside 0 .. V - 1 is rejected, leaving r as it is
  *   parents [B, T]    int32  as for the attention, but a node without a parent is never reached (but node

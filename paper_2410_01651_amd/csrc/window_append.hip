@@ -11,7 +11,8 @@
 // Bound: few tokens by the trips to memory; many by HBM, at 2 B Hkv T (64 (e + 1) + 4) bytes: four prompts of
 // up to 8,192 tokens, 16 heads, 113 MB in 22.7 us, 5.0 TB/s, as a large copy, where the last cache still has
 // what was just computed, and 121 MB in 30.6 us, 3.9 TB/s, where it has not.  (Loads that leave that cache alone:
-// 27.0 us there, but 25.6 for the 22.7.)
+// 27.0 us there, but 25.6 for the 22.7.)  The same prompts in int8 23 us, of fp32 tensors 31 (int8 32), without a window's
+// end 24 (33).
 //
 // Keep.  One wave per (sequence, cached head), eight tokens at a time (64 sequences' paths, 16 heads, 6.9 us for
 // 15.3 one by one); lane d moves key d and value d of each token.  As a path ascends, token i comes from a place at
@@ -27,7 +28,8 @@ namespace {
 
 constexpr int kAppendWaves = 8;
 // Eight tokens to a wave / a tile to a wave: 64 sequences, 16 heads, 25 tokens 6.3 / 11.5 us, 64 tokens 10.4 / 13.5, 128
-// tokens 16.6 / 16.7, 512 tokens 56 / 38; 4 sequences, 8 heads, 128 tokens 4.2 / 6.1.
+// tokens 16.6 / 16.7, 512 tokens 56 / 38; 4 sequences, 8 heads, 128 tokens 4.2 / 6.1.  (The border is where large batches
+// meet; small ones pay for it up to some hundred tokens: of 129, by tiles, 4 sequences take 6.5 us, one 5.7.)
 constexpr int64_t kFewTokens = 128;
 constexpr int kRingTile = kS * kD;  // bytes of a tile's keys or values
 

@@ -16,7 +16,7 @@
 // l = W g + c having query row c as its column, the rows of N in the order that makes a lane's
 // accumulators consecutive tokens, so that P is the second product's operand as it stands, and a tile is
 // 4 loads of 16 bytes per lane straight into registers.  Scales come one token per lane and are
-// handed round through 512 bytes of LDS per wave.
+// handed round through 768 bytes of LDS per wave (keys', values', and which are NaN).
 //
 // Work.  One item per (sequence, cached head, block of rows); its waves, of one or more workgroups, take the
 // tiles in turn and leave (m, l, out) to be joined, by the workgroup through LDS, and for several workgroups by
@@ -25,9 +25,10 @@
 // Bound.  Few rows per cached head (single tokens, small trees): HBM, 136 bytes per token and cached head.  One
 // token of 64 sequences, 16 heads, a window of 512: 15 us (71.6 MB, 4.8 TB/s); of four sequences of up to 120,000
 // tokens, 8 cached heads for 32: 76 us (411 MB, 5.4 TB/s).  Many rows (prompts): instruction issue, of which the
-// softmax has most: a tile of 64 x 64 takes 610 vector instructions beside its 32 MFMA.  8,192 tokens of 4
-// sequences, 16 heads, a window of 512: 125 us, vector pipes busy 68 %, MFMA 24 %.  A tree of 25 nodes over 8 cached heads for 32 heads, 16
-// sequences of up to 7,777 tokens: 41 us; four blocks of 32 rows unpack each tile, and vector pipes are busy 33 %.
+// softmax has most: a tile of 64 x 64 takes 490 vector instructions beside its 32 MFMA (the mean over waves of 220
+// tiles).  8,192 tokens of 4 sequences, 16 heads, a window of 512, 9 tiles per wave, two of them masked: 127 us, vector
+// pipes busy 69 %, MFMA 24 %.  A tree of 25 nodes over 8 cached heads for 32 heads, 16
+// sequences of up to 7,777 tokens: 42 us; four blocks of 32 rows unpack each tile, and vector pipes are busy 33 %.
 // One sequence's token of 8 heads over 512: 6 us, the trips to memory (length, tile, parts) one after the other.
 #include "gca_device.hpp"
 #include "gca_launch.hpp"
